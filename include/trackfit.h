@@ -423,6 +423,157 @@ int64_t tf_mingru_noalloc_max_rows(const tf_mingru *h);
  * (TF_DEVERR_* bits).  Synchronises stream. */
 tf_status tf_mingru_device_error(const tf_mingru *h, hipStream_t stream, int32_t *flags, int clear);
 
+/*
+ * Operators of the sequence layers that the paper's ablation sets beside the
+ * minGRU (Sec. Ablation: Mamba-2 and Transformer encoders): linear attention with
+ * a decay for each head over packed sequences, queries and keys normalised and
+ * rotated in front of it, and the gated feed-forward block behind it, each with its
+ * backward pass.  They take tensors rather than weight handles.  Every call is
+ * asynchronous on stream, allocates nothing and can be captured in a HIP graph;
+ * scratch memory comes from the caller (its contents need no clearing), and calls
+ * that may overlap in time need workspaces of their own.  Results do not depend on
+ * the order in which workgroups run.
+ *
+ * Tensors are row-major with unit stride inside a row ([heads][width] of a row are
+ * contiguous); row strides are in elements.  Pointers of tensors and workspaces and
+ * the rows' strides in bytes are multiples of 16 (workspaces of tf_decay_*: 256);
+ * anything else is TF_EINVAL.  Outputs must not overlap inputs unless said so.
+ * All calls: TF_EINVAL (null pointers that are needed, negative sizes, strides
+ * below a row's width, alignment, unknown element type, a workspace that is too
+ * small), TF_EUNSUPPORTED (sizes outside the supported set), TF_EHIP.
+ */
+typedef enum { TF_ELEM_FP32 = 0, TF_ELEM_BF16 = 1, TF_ELEM_FP16 = 2 } tf_elem;
+
+/* Bit of the operators' flags: offsets that decrease or leave [0, n_rows]. */
+#define TF_SEQ_BAD_OFFSETS 1
+
+/*
+ * Linear attention with a decay for each head over packed sequences: per sequence
+ * and head, from a zero (or given) state,
+ *   S_t = exp(g_t) S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t.
+ * Queries and keys have n_qk_heads heads, each used by n_heads / n_qk_heads
+ * consecutive heads; values, decays, states and outputs have n_heads.
+ * Log decays are meant to be <= 0; below about -104 (-inf too) a row forgets all
+ * before it.  reverse = 1: t runs from each sequence's last row to its first.
+ * Supported: d_k and d_v 32, 64 or 128, up to 1024 heads.
+ * fp32 tensors: products and sums in fp32.  bf16: states, decays and sums in fp32;
+ * the weights exp(b_t - b_s) q_t k_s of the values inside a chunk of 64 rows are
+ * rounded to bf16.  fp16: as fp32, rounded once at the store.
+ * A value that is infinite or NaN reaches the later rows of its own sequence only.
+ */
+typedef struct {
+    int32_t elem;        /* tf_elem of q, k, v, out and their gradients */
+    int32_t n_heads;
+    int32_t n_qk_heads;  /* divides n_heads */
+    int32_t d_k;
+    int32_t d_v;
+    int32_t reverse;     /* 0 or 1 */
+    float scale;
+} tf_decay_config;
+
+/* Bytes of workspace of tf_decay_attention and of its backward pass (0 if invalid). */
+size_t tf_decay_workspace_size(const tf_decay_config *cfg, int64_t n_rows);
+size_t tf_decay_backward_workspace_size(const tf_decay_config *cfg, int64_t n_rows, int32_t n_seqs, int32_t with_d_state);
+
+/*
+ * q, k           device, [n_rows][n_qk_heads][d_k].
+ * v              device, [n_rows][n_heads][d_v].
+ * log_decay      device, float32: rows of n_heads, decay_stride apart, or with
+ *                decay_stride 0 one value a head for all rows.
+ * offsets        device, int32 [n_seqs + 1]: sequence i owns rows offsets[i] ..
+ *                offsets[i+1]-1, as for fit_tracks.  Offsets that decrease or
+ *                leave [0, n_rows] set TF_SEQ_BAD_OFFSETS in *flags and make
+ *                every output NaN.
+ * initial_state  device, float32 [n_seqs][n_heads][d_k][d_v], or NULL for zeros.
+ * out            device, [n_rows][n_heads][d_v].  Rows outside of all sequences are
+ *                not written.
+ * final_state    device, float32, as initial_state, or NULL.  A sequence without
+ *                rows passes its initial state on.
+ * flags          device int32 or NULL, OR-ed.
+ */
+tf_status tf_decay_attention(const tf_decay_config *cfg, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                             const void *v, int64_t v_stride, const float *log_decay, int64_t decay_stride, int64_t n_rows,
+                             const int32_t *offsets, int32_t n_seqs, const float *initial_state, void *workspace,
+                             size_t workspace_bytes, void *out, int64_t out_stride, float *final_state, int32_t *flags,
+                             hipStream_t stream);
+
+/*
+ * Gradients of tf_decay_attention's inputs from those of its outputs: d_out as out,
+ * d_state as final_state (NULL: the last states are not used).  dq, dk, dv as q, k, v
+ * (queries and keys that heads share get the sum); d_log_decay float32
+ * [n_rows][n_heads], or [n_heads] with decay_stride 0 (the sum over all rows);
+ * d_initial as initial_state, or NULL.  Other arguments are those of the forward call.
+ */
+tf_status tf_decay_attention_backward(const tf_decay_config *cfg, const void *d_out, int64_t d_out_stride, const void *q,
+                                      int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                                      const float *log_decay, int64_t decay_stride, int64_t n_rows, const int32_t *offsets,
+                                      int32_t n_seqs, const float *initial_state, const float *d_state, void *workspace,
+                                      size_t workspace_bytes, void *dq, int64_t dq_stride, void *dk, int64_t dk_stride,
+                                      void *dv, int64_t dv_stride, float *d_log_decay, float *d_initial, int32_t *flags,
+                                      hipStream_t stream);
+
+/*
+ * One row of each of n_seqs sequences, for serving: q, k [n_seqs][n_qk_heads][d_k],
+ * v and out [n_seqs][n_heads][d_v], log_decay [n_seqs] rows (decay_stride 0: one
+ * value a head), states float32 [n_seqs][n_heads][d_k][d_v].  state_out may be state
+ * (updated in place) or must not overlap it.  cfg->reverse has no meaning here.
+ */
+tf_status tf_decay_attention_step(const tf_decay_config *cfg, const void *q, int64_t q_stride, const void *k,
+                                  int64_t k_stride, const void *v, int64_t v_stride, const float *log_decay,
+                                  int64_t decay_stride, int32_t n_seqs, const float *state, float *state_out, void *out,
+                                  int64_t out_stride, hipStream_t stream);
+
+/*
+ * Queries and keys normalised per head and rotated by position, in one pass:
+ *   n = x / sqrt(mean(x^2) + eps) * gain            (each head; gains shared by the heads)
+ *   (lo, hi) -> (lo cos a - hi sin a, lo sin a + hi cos a),  a = position base^(-2 j / rotary_dim)
+ * for pairs j < rotary_dim / 2: values j and j + rotary_dim / 2, or (interleaved)
+ * 2 j and 2 j + 1.  Values from rotary_dim on are only normalised.
+ * Sums and products in fp32, angles in fp64, one rounding at the store.
+ * Supported: head_dim 32, 64, 128 or 256, rotary_dim a multiple of 16 up to it.
+ */
+typedef struct {
+    int32_t elem;        /* tf_elem of q, k, the outputs and their gradients */
+    int32_t n_q_heads;
+    int32_t n_k_heads;
+    int32_t head_dim;
+    int32_t rotary_dim;
+    int32_t interleaved; /* 0 or 1 */
+    float eps;
+    double base;
+} tf_qk_norm_config;
+
+/*
+ * q, k      device, [n_rows][heads][head_dim].
+ * gains     device, float32 [head_dim].
+ * positions device, int32 [n_rows], or NULL: then a row's position counts from its
+ *           sequence's first row (offsets given) or from row 0.
+ * offsets   device, int32 [n_seqs + 1], or NULL: with offsets, only rows offsets[0] ..
+ *           offsets[n_seqs]-1 are read and written.  Offsets out of order give some
+ *           positions no meaning.
+ * q_out, k_out  as q, k; may be q and k themselves (same stride).
+ */
+tf_status tf_qk_norm_rotate(const tf_qk_norm_config *cfg, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                            int64_t n_rows, const float *q_gain, const float *k_gain, const int32_t *positions,
+                            const int32_t *offsets, int32_t n_seqs, void *q_out, int64_t q_out_stride, void *k_out,
+                            int64_t k_out_stride, hipStream_t stream);
+
+/* Bytes of workspace of the backward pass (0 if invalid). */
+size_t tf_qk_norm_workspace_size(const tf_qk_norm_config *cfg, int64_t n_rows);
+
+/*
+ * Gradients of q, k (dq, dk; may be dq_out and dk_out themselves with the same
+ * stride) and of the gains (float32 [head_dim], sums over the rows and heads) from
+ * those of the outputs (dq_out, dk_out).  Other arguments are those of the forward
+ * call, whose q and k these are.
+ */
+tf_status tf_qk_norm_rotate_backward(const tf_qk_norm_config *cfg, const void *dq_out, int64_t dq_out_stride,
+                                     const void *dk_out, int64_t dk_out_stride, const void *q, int64_t q_stride,
+                                     const void *k, int64_t k_stride, int64_t n_rows, const float *q_gain,
+                                     const float *k_gain, const int32_t *positions, const int32_t *offsets,
+                                     int32_t n_seqs, void *workspace, size_t workspace_bytes, void *dq, int64_t dq_stride,
+                                     void *dk, int64_t dk_stride, float *dq_gain, float *dk_gain, hipStream_t stream);
+
 /* Static description of a status code (library plumbing: no passage of the
  * paper defines it). */
 const char *tf_status_string(tf_status s);

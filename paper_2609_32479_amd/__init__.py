@@ -12,7 +12,10 @@ import os
 
 import torch  # noqa: F401  -- load torch's HIP runtime before the library (one runtime per process)
 
-__all__ = ["LIB_PATH", "Config", "Weights", "fit_tracks", "device_error", "blob_size",
+from . import operators
+from .operators import *  # noqa: F401,F403
+
+__all__ = [*operators.__all__, "LIB_PATH", "Config", "Weights", "fit_tracks", "device_error", "blob_size",
            "TF_FP32", "TF_BF16", "TF_BF16_F16ACT", "DTYPES", "MODE_FOR_WEIGHTS", "DEVERR_EMPTY_TRACK", "DEVERR_TOO_LONG", "DEVERR_BAD_OFFSETS", "DEVERR_PAIR",
            "TrackfitError", "lib", "seed_tracks", "fit_tracks_states", "Readout", "decode_tracks",
            "readout_blob_size", "MinGRU", "MinGRUConfig", "SEED_TOO_SHORT", "SEED_NO_CIRCLE", "SEED_BAD_OFFSETS"]
@@ -33,7 +36,7 @@ EXPORTED = ("tf_weights_create", "tf_weights_destroy", "tf_blob_size", "tf_fouri
             "tf_readout_blob_size", "tf_readout_create", "tf_readout_destroy", "tf_decode_tracks",
             "tf_mingru_blob_size", "tf_mingru_create", "tf_mingru_destroy", "tf_mingru_workspace_size",
             "tf_mingru_states", "tf_mingru_device_error", "tf_mingru_states_noalloc", "tf_mingru_noalloc_max_rows",
-            "tf_mingru_set_fused")
+            "tf_mingru_set_fused", *operators.EXPORTED)
 
 
 class TrackfitError(RuntimeError):
@@ -111,6 +114,7 @@ def lib():
         L.tf_mingru_device_error.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_int32), ctypes.c_int]
         L.tf_decode_tracks.restype = ctypes.c_int
         L.tf_decode_tracks.argtypes = [vp, ctypes.c_int32, vp, vp, vp, vp, vp]
+        operators.declare(L)
         _lib = L
     return _lib
 

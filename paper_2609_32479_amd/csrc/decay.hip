@@ -1,0 +1,1095 @@
+// Linear attention with a decay for each head over packed sequences (gfx950):
+//
+//   S_t = exp(g_t) S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t            (each sequence and head)
+//
+// with its backward pass and its form for single tokens.  In chunks of 64 rows,
+// with b the running sum of g,
+//
+//   o_t = scale (sum over s <= t of exp(b_t - b_s) (q_t k_s) v_s  +  exp(b_t) S_in^T q_t)
+//   S_out = exp(b_end) S_in + sum over s of exp(b_end - b_s) k_s v_s^T
+//
+// so that all of it is matrix products.  Only differences b_t - b_s within one
+// sequence are ever exponentiated; with g <= 0 none of them overflows.
+//
+// The gradients are the same function of other arguments: with U_t the gradient
+// of S_t, which runs the other way,
+//
+//   dq_t = scale S_t do_t                                 q, k, v <- do, v, k    (S transposed)
+//   dv_s = U_s^T k_s                                      q, k, v <- k, q, do    (from the last row)
+//   dk_s = U_s v_s                                        q, k, v <- v, do, q    (from the last row)
+//   U_s = scale q_s do_s^T + exp(g_{s+1}) U_{s+1}
+//
+// (in that direction a row's decay is its predecessor's: `shift`), and with
+// db_t = q_t dq_t - k_t dk_t the gradient of g_t is the sum of db over the
+// sequence's rows from t on, plus <dS_last, S_last>.
+//
+// How the rows are split.  Sequences may be a handful of rows or tens of
+// thousands, and the host does not know their lengths.  So the packed rows are cut
+// into spans of equal length, whatever sequences they hold: chunks of a span hold
+// rows of several sequences, whose products are masked apart.  A span border within
+// 64 rows of an end of its sequence moves there; only the others cut a sequence, and
+// for these a first launch computes each span's own contribution to the state at its
+// end, and a second joins them in order.  With tracks of up to 64 hits no border
+// cuts a sequence and these two launches end at once.
+//
+// Numbers.  bf16 tensors: the products q k^T, and the states' products, take bf16
+// operands that are the tensors themselves, or fp32 values as three bf16 parts (two
+// where the result is only rounded to bf16), so that states, decays and everything
+// that reaches the decays' gradient are fp32; the weights exp(b_t - b_s) (q_t k_s)
+// are rounded once to bf16 to multiply v.  fp32 and fp16 tensors are multiplied by the
+// fp32 instruction.
+#include "ops.h"
+
+#include <cmath>
+
+namespace {
+
+constexpr int kChunk = 64;
+constexpr int kMinSpan = 2 * kChunk;  // borders move by less than a chunk: their order stays
+constexpr float kForget = -200.0f;    // exp of this and less is 0: smaller log decays, -inf too, count as it
+typedef __attribute__((ext_vector_type(4))) short o_s16x4;
+typedef __attribute__((ext_vector_type(4))) __bf16 o_bf16x4;
+typedef __attribute__((ext_vector_type(8))) __bf16 o_bf16x8;
+typedef __attribute__((ext_vector_type(4))) _Float16 o_f16x4;
+typedef __attribute__((address_space(3))) o_s16x4 lds_s16x4;
+
+// The matrix-core side.  A fragment of an operand is 16 bytes a lane: row (or column) lane % 16,
+// and 8 (bf16) or 4 (fp32) of KM values along the sum for the lane group lane / 16.
+struct MatBF16 {
+    typedef __bf16 E;
+    typedef o_bf16x8 F;
+    static constexpr int KM = 32, PAD = 8;
+    static __device__ __forceinline__ o_f32x4 mma(F a, F b, o_f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+    // the sum runs along x's rows: x[row][k0 ..]
+    static __device__ __forceinline__ F along(const E *x, int ld, int row, int k0, int q) {
+        return *(const F *)(x + row * ld + k0 + 8 * q);
+    }
+    // the sum runs down x's columns: x[k0 ..][c0 + lane % 16], read transposed
+    static __device__ __forceinline__ F down(const E *x, int ld, int k0, int c0, int n, int q) {
+        const E *p = x + (k0 + 8 * q + n / 4) * ld + c0 + 4 * (n % 4);
+        const o_s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
+        const o_s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 4 * ld));
+        return __builtin_bit_cast(F, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    // x[row][k0 ..] in the order in which the accumulators of a state hold those rows
+    static __device__ __forceinline__ F along_state(const E *x, int ld, int row, int k0, int q) {
+        const o_bf16x4 a = *(const o_bf16x4 *)(x + row * ld + k0 + 4 * q);
+        const o_bf16x4 b = *(const o_bf16x4 *)(x + row * ld + k0 + 16 + 4 * q);
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    static constexpr int TILES = 2;  // state tiles of 16 rows in a fragment
+    // c += a b for fp32 values a (N bf16 parts, the small ones first)
+    template <int N> static __device__ __forceinline__ void split(const float *x, F (&p)[N]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float r = x[i];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                p[j][i] = (__bf16)r;
+                r -= (float)p[j][i];
+            }
+        }
+    }
+};
+struct MatF32 {
+    typedef float E;
+    typedef o_f32x4 F;
+    static constexpr int KM = 16, PAD = 4;
+    static __device__ __forceinline__ o_f32x4 mma(F a, F b, o_f32x4 c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+        return c;
+    }
+    static __device__ __forceinline__ F along(const E *x, int ld, int row, int k0, int q) {
+        return *(const F *)(x + row * ld + k0 + 4 * q);
+    }
+    static __device__ __forceinline__ F down(const E *x, int ld, int k0, int c0, int n, int q) {
+        F f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = x[(k0 + 4 * q + i) * ld + c0 + n];
+        return f;
+    }
+    static __device__ __forceinline__ F along_state(const E *x, int ld, int row, int k0, int q) {
+        return along(x, ld, row, k0, q);
+    }
+    static constexpr int TILES = 1;
+    template <int N> static __device__ __forceinline__ void split(const float *x, F (&p)[N]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[0][i] = x[i];
+    }
+};
+// How many parts an fp32 operand needs for `n` bf16 parts' worth of digits.
+template <class M> constexpr int parts_of(int n) { return M::KM == 32 ? n : 1; }
+template <class T> struct MatOf { typedef MatF32 M; };
+template <> struct MatOf<ElemBF16> { typedef MatBF16 M; };
+
+// Where the spans' borders are.
+struct Spans {
+    const int2 *info;  // first and past-the-last row of each row's sequence, (-1, -1) outside of all
+    int n_rows, span, n;
+    struct Border {
+        int row;
+        bool cuts;  // rows row - 1 and row are of one sequence
+    };
+    __device__ __forceinline__ Border border(int p) const {
+        if (p <= 0) return {0, false};
+        const long long b = (long long)p * span;
+        if (p >= n || b >= n_rows) return {n_rows, false};
+        const int r = (int)b;
+        const int2 s = info[r];
+        if (s.x < 0 || s.x == r) return {r, false};
+        if (r - s.x < kChunk) return {s.x, false};
+        if (s.y - r < kChunk) return {s.y, false};
+        return {r, true};
+    }
+};
+
+struct DecayRun {
+    const void *q, *k, *v, *x;           // x: what the part from the state is multiplied with for db
+    long long qs, ks, vs, xs;            // row strides, elements
+    int qg, kg, vg, xg;                  // heads that share one of these
+    void *out;
+    long long os;
+    int out_f32;                         // out holds fp32 rows of all heads (summed over sharing heads later)
+    const float *g;
+    long long gs;                        // 0: one decay a head
+    int shift;
+    const float *s0;                     // [n_seqs][heads][state], or null
+    float *sf;
+    int turned;                          // states in memory are the transposed of this run's
+    int sf_decay;                        // the last state is multiplied by the last row's own decay
+    float *local;                        // [spans][heads][state]: the state at the spans' ends
+    float *mult;                         // [spans][heads]: decay over a span that is all one sequence's
+    int *kind;                           // [spans]: 0 its end cuts no sequence, 1 it does, 2 and its start cuts the same
+    float *db;                           // [n_rows][heads]
+    float out_scale, kv_scale;
+    const int32_t *offsets;
+    int n_seqs, heads, dir;
+    const int *bad;
+    Spans spans;
+};
+
+enum { DECAY_STATE = 0, DECAY_OUT = 1, DECAY_DOT = 2, DECAY_PAIRS = 3 };
+
+__device__ __forceinline__ float log_decay_of(const DecayRun &A, int r, int h) {
+    const float g = A.gs ? A.g[(long long)r * A.gs + h] : A.g[h];
+    return g < kForget ? kForget : g;  // (NaN stays)
+}
+
+// The 16-byte pieces of a [64][D] tile that a thread brings from memory to LDS.
+template <class T, class M, int D, int NT> struct Tile {
+    typedef typename T::E E;
+    typedef typename M::E ME;
+    static constexpr int VEC = 16 / sizeof(E), PIECES = D / VEC, ALL = kChunk * PIECES, N = (ALL + NT - 1) / NT;
+    o_u32x4 raw[N];
+    // rows row0 + dir * i, i < rows, inside [lo, hi); zeros for the others
+    __device__ __forceinline__ void load(const void *base, long long stride, int col, int row0, int dir, int rows, int lo,
+                                         int hi, int tid) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int c = tid + j * NT, i = c / PIECES, r = row0 + dir * i;
+            raw[j] = o_u32x4{0, 0, 0, 0};
+            if (c < ALL && i < rows && r >= lo && r < hi)
+                raw[j] = *(const o_u32x4 *)((const E *)base + (long long)r * stride + col + (c % PIECES) * VEC);
+        }
+    }
+    __device__ __forceinline__ void store(ME *lds, int tid) const {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int c = tid + j * NT;
+            if (ALL % NT && c >= ALL) break;
+            ME *p = lds + (c / PIECES) * (D + M::PAD) + (c % PIECES) * VEC;
+            if constexpr (sizeof(ME) == sizeof(E)) {
+                *(o_u32x4 *)p = raw[j];
+            } else {  // fp16 to fp32
+                typedef __attribute__((ext_vector_type(8))) _Float16 H8;
+                *(o_f32x8 *)p = __builtin_convertvector(__builtin_bit_cast(H8, raw[j]), o_f32x8);
+            }
+        }
+    }
+    __device__ __forceinline__ bool infinite() const {  // or NaN
+        unsigned bad = 0;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const unsigned u = raw[j][w];
+                if constexpr (sizeof(E) == 4) {
+                    bad |= (u & 0x7fffffffu) >= 0x7f800000u;
+                } else {
+                    constexpr unsigned top = sizeof(ME) == 2 ? 0x7f80u : 0x7c00u;
+                    bad |= (u & 0x7fffu) >= top;
+                    bad |= ((u >> 16) & 0x7fffu) >= top;
+                }
+            }
+        return bad != 0;
+    }
+};
+
+template <class T> __device__ __forceinline__ void store4(typename T::E *p, o_f32x4 v) {
+    typedef __attribute__((ext_vector_type(4))) typename T::E V;
+    *(V *)p = __builtin_convertvector(v, V);
+}
+
+// One span of one head.  Waves: each owns 16 of the state's and the output's columns; the state
+// stays in its accumulators over the span.  The 64 x 64 weights of a chunk are computed once,
+// 16 x 16 tiles on or below the diagonal dealt out to the waves, and pass through LDS.
+template <class T, int DK, int DV, int MODE>
+__global__ __launch_bounds__(4 * DV) void tf_decay_span_kernel(DecayRun A) {
+    typedef typename MatOf<T>::M M;
+    typedef typename M::E ME;
+    typedef typename M::F F;
+    constexpr bool OUT = MODE >= DECAY_OUT, DOT = MODE >= DECAY_DOT, PAIRS = MODE == DECAY_PAIRS;
+    constexpr int NW = DV / 16, NT = 64 * NW, KM = M::KM;
+    constexpr int LK = DK + M::PAD, LV = DV + M::PAD, LP = kChunk + M::PAD;
+    constexpr int ST = DK / 16;                    // state tiles of a wave
+    constexpr int NB = kChunk / KM;                // fragments along a chunk's rows
+    constexpr int NS = parts_of<M>(DOT ? 3 : 2);   // parts of the state in its product with q
+    constexpr int NU = parts_of<M>(3);             // parts of the weighted v in the state's update
+    __shared__ __attribute__((aligned(16))) ME Qs[OUT ? kChunk * LK : 8], Ks[kChunk * LK], Vs[kChunk * LV],
+        Xs[DOT ? kChunk * LV : 8], Ps[OUT ? kChunk * LP : 8];
+    __shared__ float bh[kChunk], bl[kChunk], fo[kChunk], wt[kChunk], endd[kChunk];
+    __shared__ int first[kChunk], past[kChunk], stat[kChunk];
+    __shared__ float rowp[PAIRS ? 4 : 1][kChunk], colp[PAIRS ? 4 : 1][kChunk], dots[DOT ? NW : 1][kChunk];
+
+    const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+    const int n = lane % 16, q = lane / 16, c0 = 16 * wave;
+    const int p = blockIdx.x / A.heads, h = blockIdx.x % A.heads, dir = A.dir;
+    if (*A.bad) {
+        if (OUT) {  // offsets that make no sequences: every row of the array is NaN
+            const long long lo = (long long)p * A.spans.span;
+            const long long hi = lo + A.spans.span < A.spans.n_rows ? lo + A.spans.span : A.spans.n_rows;
+            const float nan = __builtin_nanf("");
+            for (long long r = lo; r < hi; ++r)
+                for (int i = tid; i < DV; i += NT) {
+                    if (A.out_f32) ((float *)A.out)[r * A.os + h * DV + i] = nan;
+                    else ((typename T::E *)A.out)[r * A.os + h * DV + i] = (typename T::E)nan;
+                }
+        }
+        return;
+    }
+    const Spans::Border b0 = A.spans.border(p), b1 = A.spans.border(p + 1);
+    int lo = b0.row, hi = b1.row;
+    const bool cut_in = dir > 0 ? b0.cuts : b1.cuts, cut_out = dir > 0 ? b1.cuts : b0.cuts;
+    bool whole = false;
+    if (!OUT) {
+        // only the sequence that the span's end cuts has a state there
+        int kind = 0;
+        if (cut_out) {
+            const int2 s = A.spans.info[dir > 0 ? hi - 1 : lo];
+            whole = cut_in && (dir > 0 ? s.x < lo : s.y > hi);
+            kind = whole ? 2 : 1;
+            if (dir > 0) lo = s.x > lo ? s.x : lo;
+            else hi = s.y < hi ? s.y : hi;
+        }
+        if (h == 0 && tid == 0) A.kind[p] = kind;
+        if (!cut_out) return;
+    }
+    if (hi <= lo) return;
+    // Chunks are counted from the span's first row in memory whichever way they are run through, so that the runs of
+    // both directions have the same ones (db's two halves are split by chunks).
+    const int chunks = (hi - lo + kChunk - 1) / kChunk;
+    const int olo = A.offsets[0], ohi = A.offsets[A.n_seqs];
+
+    o_f32x4 S[ST];
+#pragma unroll
+    for (int m = 0; m < ST; ++m) S[m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
+    bool have = false;  // the state is that of the sequence that goes on
+    auto load_state = [&](const float *s) {
+#pragma unroll
+        for (int m = 0; m < ST; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int a = 16 * m + 4 * q + i, b = c0 + n;
+                S[m][i] = A.turned ? s[b * DK + a] : s[a * DV + b];
+            }
+    };
+    if (OUT && cut_in) {
+        load_state(A.local + ((long long)(p - dir) * A.heads + h) * (DK * DV));
+        have = true;
+    }
+    if (OUT) {  // the weights above the diagonal that share a fragment with some below
+        for (int i = tid; i < kChunk * LP; i += NT) Ps[i] = (ME)0.0f;
+    }
+
+    Tile<T, M, DK, NT> tq, tk;
+    Tile<T, M, DV, NT> tv, tx;
+    const int hq = h / A.qg * DK, hk = h / A.kg * DK, hv = h / A.vg * DV, hx = DOT ? h / A.xg * DV : 0;
+    auto chunk_at = [&](int c, int &row0, int &rows) {  // the c-th chunk on the way: its first row on the way, its rows
+        const int at = lo + (dir > 0 ? c : chunks - 1 - c) * kChunk;
+        rows = hi - at < kChunk ? hi - at : kChunk;
+        row0 = dir > 0 ? at : at + rows - 1;
+    };
+    auto fetch = [&](int c) {
+        int row0, rows;
+        chunk_at(c, row0, rows);
+        if (OUT) tq.load(A.q, A.qs, hq, row0, dir, rows, olo, ohi, tid);
+        tk.load(A.k, A.ks, hk, row0, dir, rows, olo, ohi, tid);
+        tv.load(A.v, A.vs, hv, row0, dir, rows, olo, ohi, tid);
+        if (DOT) tx.load(A.x, A.xs, hx, row0, dir, rows, olo, ohi, tid);
+    };
+    fetch(0);
+    double total = 0.0;
+
+    for (int c = 0; c < chunks; ++c) {
+        int row0, rows;
+        chunk_at(c, row0, rows);
+        if (OUT) tq.store(Qs, tid);
+        tk.store(Ks, tid);
+        tv.store(Vs, tid);
+        if (DOT) tx.store(Xs, tid);
+        const int wild = tk.infinite() || tv.infinite();
+        if (wave == 0) {
+            // The chunk's rows: where their sequences begin and end in it, and the sums of their log decays from there.
+            const int i = lane, r = row0 + dir * i;
+            const int2 s = i < rows ? A.spans.info[r] : int2{-1, -1};
+            const bool live = s.x >= 0;
+            int f = i, l = i;
+            if (live) f = dir > 0 ? s.x - row0 : row0 - (s.y - 1), l = dir > 0 ? s.y - 1 - row0 : row0 - s.x;
+            double b = 0.0;
+            if (live && !(A.shift && f == i)) b = (double)log_decay_of(A, A.shift ? r - dir : r, h);
+            const int from = f > 0 ? f : 0;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const double o = __shfl_up(b, d);
+                if (i - d >= from) b += o;
+            }
+            const int e = l < rows - 1 ? l : rows - 1;
+            const double be = __shfl(b, e & 63), w = be - b;
+            const float bf = (float)b, bg = (float)(b - (double)bf), wf = (float)w, wg = (float)(w - (double)wf);
+            bh[i] = bf, bl[i] = bg;
+            const float eb = expf(bf), ew = expf(wf);
+            fo[i] = A.out_scale * (eb + eb * bg);
+            wt[i] = A.kv_scale * (ew + ew * wg);
+            endd[i] = eb + eb * bg;
+            first[i] = live ? f : 64;
+            past[i] = live ? e + 1 : i + 1;
+            stat[i] = (live ? 1 : 0) | (live && l <= rows - 1 ? 2 : 0);
+            total += __shfl(b, rows - 1);
+        }
+        const bool slow = __syncthreads_or(wild);
+        if (c + 1 < chunks) fetch(c + 1);
+
+        if (OUT) {
+            // weights: tile (s tile ms, t tile mt), transposed, so that four consecutive s of a row t land in a lane
+            constexpr int tiles = 10;
+            for (int w = wave; w < tiles; w += NW) {
+                const int mt = w < 4 ? 3 : w < 7 ? 2 : w < 9 ? 1 : 0, ms = w < 4 ? w : w < 7 ? w - 4 : w < 9 ? w - 7 : 0;
+                o_f32x4 a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k0 = 0; k0 < DK; k0 += KM)
+                    a = M::mma(M::along(Ks, LK, 16 * ms + n, k0, q), M::along(Qs, LK, 16 * mt + n, k0, q), a);
+                const int t = 16 * mt + n, s = 16 * ms + 4 * q, f = first[t];
+                const float th = bh[t], tl = bl[t];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float e = A.out_scale * A.kv_scale * expf((th - bh[s + i]) + (tl - bl[s + i]));
+                    a[i] = s + i <= t && s + i >= f ? a[i] * e : 0.0f;
+                }
+                typedef __attribute__((ext_vector_type(4))) ME V4;
+                *(V4 *)(Ps + t * LP + s) = __builtin_convertvector(a, V4);
+                if (PAIRS) {
+                    // products of dq's weights with q k: their sums by t and by s are what q dq and k dk have of them
+                    o_f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int k0 = 0; k0 < DV; k0 += KM)
+                        z = M::mma(M::along(Vs, LV, 16 * ms + n, k0, q), M::along(Xs, LV, 16 * mt + n, k0, q), z);
+                    float col[4], row = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        col[i] = s + i <= t && s + i >= f ? a[i] * z[i] : 0.0f;
+                        row += col[i];
+                    }
+                    row += __shfl_xor(row, 16);
+                    row += __shfl_xor(row, 32);
+                    if (q == 0) rowp[ms][t] = row;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                        for (int d = 1; d < 16; d *= 2) col[i] += __shfl_xor(col[i], d);
+                        if (n == 0) colp[mt][s + i] = col[i];
+                    }
+                }
+            }
+            __syncthreads();
+        }
+
+        o_f32x4 o[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) o[m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
+        // The chunk's sequences, one after the other: what their state adds to their rows, and the state after them.
+        for (int a = 0; a < rows;) {
+            const int b = __builtin_amdgcn_readfirstlane(past[a]), st = __builtin_amdgcn_readfirstlane(stat[a]);
+            if (!(st & 1)) {
+                a = b;
+                continue;
+            }
+            const bool starts = __builtin_amdgcn_readfirstlane(first[a]) == a, ends = st & 2;
+            int seq = -1;
+            if ((starts && A.s0) || (ends && A.sf)) seq = seq_of_row(A.offsets, A.n_seqs, row0 + dir * a);
+            if (starts) {
+                have = A.s0 != nullptr;
+                if (have) load_state(A.s0 + ((long long)seq * A.heads + h) * (DK * DV));
+            }
+            if (OUT && have) {
+                F sp[DK / KM][NS];
+#pragma unroll
+                for (int k = 0; k < DK / KM; ++k) {
+                    float x[4 * M::TILES];
+#pragma unroll
+                    for (int i = 0; i < 4 * M::TILES; ++i) x[i] = S[k * M::TILES + i / 4][i % 4];
+                    M::template split<NS>(x, sp[k]);
+                }
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    if (16 * m + 16 <= a || 16 * m >= b) continue;
+                    o_f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int k = 0; k < DK / KM; ++k) {
+                        const F f = M::along_state(Qs, LK, 16 * m + n, k * KM, q);
+#pragma unroll
+                        for (int j = NS - 1; j >= 0; --j) z = M::mma(sp[k][j], f, z);
+                    }
+                    const int t = 16 * m + n;
+                    const float f = fo[t];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[m][i] = t >= a && t < b ? z[i] * f : o[m][i];
+                }
+            }
+            if (!ends || A.sf) {
+                const float d = endd[b - 1];
+#pragma unroll
+                for (int m = 0; m < ST; ++m) S[m] = have ? S[m] * d : o_f32x4{0.f, 0.f, 0.f, 0.f};
+                if (!slow) {
+#pragma unroll
+                    for (int k = 0; k < NB; ++k) {
+                        const F v = M::down(Vs, LV, k * KM, c0, n, q);
+                        float x[KM / 4];
+#pragma unroll
+                        for (int i = 0; i < KM / 4; ++i) {
+                            const int s = k * KM + KM / 4 * q + i;
+                            x[i] = s >= a && s < b ? (float)v[i] * wt[s] : 0.0f;
+                        }
+                        F vp[NU];
+                        M::template split<NU>(x, vp);
+#pragma unroll
+                        for (int m = 0; m < ST; ++m) {
+                            const F kf = M::down(Ks, LK, k * KM, 16 * m, n, q);
+#pragma unroll
+                            for (int j = NU - 1; j >= 0; --j) S[m] = M::mma(kf, vp[j], S[m]);
+                        }
+                    }
+                } else {
+                    for (int s = a; s < b; ++s) {
+                        const float v = (float)Vs[s * LV + c0 + n] * wt[s];
+#pragma unroll
+                        for (int m = 0; m < ST; ++m)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) S[m][i] += (float)Ks[s * LK + 16 * m + 4 * q + i] * v;
+                    }
+                }
+                have = true;
+                if (ends && A.sf) {
+                    float *s = A.sf + ((long long)seq * A.heads + h) * (DK * DV);
+                    float d = 1.0f;
+                    if (A.sf_decay) d = expf(log_decay_of(A, row0 + dir * (b - 1), h));
+#pragma unroll
+                    for (int m = 0; m < ST; ++m)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int e = 16 * m + 4 * q + i, f = c0 + n;
+                            s[A.turned ? f * DK + e : e * DV + f] = S[m][i] * d;
+                        }
+                }
+            }
+            a = b;
+        }
+        if (OUT) {
+            if (DOT) {
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    float z = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z += o[m][i] * (float)Xs[(16 * m + n) * LV + c0 + 4 * q + i];
+                    z += __shfl_xor(z, 16);
+                    z += __shfl_xor(z, 32);
+                    if (q == 0) dots[wave][16 * m + n] = z;
+                }
+            }
+            if (!slow) {
+#pragma unroll
+                for (int k = 0; k < NB; ++k) {
+                    const F v = M::down(Vs, LV, k * KM, c0, n, q);
+#pragma unroll
+                    for (int m = 0; m < 4; ++m)
+                        if (k * KM <= 16 * m) o[m] = M::mma(v, M::along(Ps, LP, 16 * m + n, k * KM, q), o[m]);
+                }
+            } else {
+                // an infinite or NaN k or v: only the products that the definition has
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    const int t = 16 * m + n, f = first[t] > 0 ? first[t] : 0;
+                    for (int s = f; s <= t; ++s)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[m][i] += (float)Ps[t * LP + s] * (float)Vs[s * LV + c0 + 4 * q + i];
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                const int t = 16 * m + n;
+                if (t < rows && (stat[t] & 1)) {
+                    const long long at = (long long)(row0 + dir * t) * A.os + h * DV + c0 + 4 * q;
+                    if (A.out_f32) *(o_f32x4 *)((float *)A.out + at) = o[m];
+                    else store4<T>((typename T::E *)A.out + at, o[m]);
+                }
+            }
+        }
+        __syncthreads();
+        if (DOT && wave == 0) {
+            const int t = lane;
+            if (t < rows && (stat[t] & 1)) {
+                float z = 0.0f;
+                for (int w = 0; w < NW; ++w) z += dots[w][t];
+                if (PAIRS)
+                    for (int m = 0; m < 4; ++m) {
+                        if (m <= t / 16) z += rowp[m][t];
+                        if (m >= t / 16) z -= colp[m][t];
+                    }
+                A.db[(long long)(row0 + dir * t) * A.heads + h] = z;
+            }
+        }
+    }
+    if (!OUT) {
+        float *s = A.local + ((long long)p * A.heads + h) * (DK * DV);
+#pragma unroll
+        for (int m = 0; m < ST; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[(16 * m + 4 * q + i) * DV + c0 + n] = S[m][i];
+        if (tid == 0) A.mult[(long long)p * A.heads + h] = whole ? expf((float)total) : 0.0f;
+    }
+}
+
+// First and past-the-last row of every row's sequence; whether the offsets are in order and inside the array.
+__global__ __launch_bounds__(256) void tf_decay_index_kernel(const int32_t *__restrict__ offsets, int n_seqs, int n_rows,
+                                                             int2 *__restrict__ info, int *__restrict__ bad,
+                                                             int32_t *__restrict__ flags) {
+    if (blockIdx.x == 0) {
+        int wrong = 0;
+        for (int i = threadIdx.x; i <= n_seqs; i += 256) {
+            const int o = offsets[i];
+            wrong |= o < 0 || o > n_rows || (i < n_seqs && offsets[i + 1] < o);
+        }
+        wrong = __syncthreads_or(wrong);
+        if (threadIdx.x == 0) {
+            *bad = wrong;
+            if (wrong && flags) atomicOr(flags, TF_SEQ_BAD_OFFSETS);
+        }
+        return;
+    }
+    const long long r = (long long)(blockIdx.x - 1) * 256 + threadIdx.x;
+    if (r >= n_rows) return;
+    const int s = seq_of_row(offsets, n_seqs, r);
+    info[r] = s < 0 ? int2{-1, -1} : int2{offsets[s], offsets[s + 1]};
+}
+
+// The states at the spans' ends from the spans' own contributions, in order along each cut sequence.
+__global__ __launch_bounds__(256) void tf_decay_chain_kernel(float *__restrict__ local, const float *__restrict__ mult,
+                                                             const int *__restrict__ kind, int n_spans, int heads, int size,
+                                                             int dir, const int *bad) {
+    if (*bad) return;
+    const int p = blockIdx.x / heads, h = blockIdx.x % heads, e = (blockIdx.y * 256 + threadIdx.x) * 4;
+    if (kind[p] != 1 || e >= size) return;  // a sequence's first cut
+    o_f32x4 s = *(const o_f32x4 *)(local + ((long long)p * heads + h) * size + e);
+    for (int i = p + dir; i >= 0 && i < n_spans && kind[i] == 2; i += dir) {
+        const long long at = (long long)i * heads + h;
+        o_f32x4 *l = (o_f32x4 *)(local + at * size + e);
+        s = *l + s * mult[at];
+        *l = s;
+    }
+}
+
+// States of sequences without rows: the first one passes through.  With bad offsets all are NaN.
+__global__ __launch_bounds__(256) void tf_decay_empty_kernel(const int32_t *__restrict__ offsets, int n_seqs, long long size,
+                                                             const float *__restrict__ s0, float *__restrict__ sf,
+                                                             const int *bad) {
+    const bool wrong = *bad;
+    for (int i = blockIdx.x; i < n_seqs; i += gridDim.x) {
+        if (!wrong && offsets[i] != offsets[i + 1]) continue;
+        for (long long e = threadIdx.x; e < size; e += 256)
+            sf[i * size + e] = wrong ? __builtin_nanf("") : s0 ? s0[i * size + e] : 0.0f;
+    }
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+    return v;
+}
+
+struct DecayGrad {
+    Spans spans;
+    const float *S, *U;          // the states and their gradients at the spans' ends
+    const float *Sl, *Ul;        // of the sequences' last rows, or null
+    float *cut, *last;           // their inner products: [spans][heads], [n_seqs][heads]
+    const float *g;
+    long long gs;
+    const float *da, *db;        // q dq - (k dk within chunks), k dk from the states
+    float *dg, *part;            // part: [spans][heads], with one decay a head
+    const int32_t *offsets;
+    int n_seqs, heads, dir, size;
+    const int *bad;
+};
+
+// Inner products of states and their gradients: a wave each, of the cut borders and of the sequences' ends.
+__global__ __launch_bounds__(256) void tf_decay_dots_kernel(DecayGrad A) {
+    if (*A.bad) return;
+    const long long item = (long long)blockIdx.x * 4 + threadIdx.x / 64, borders = (long long)A.spans.n * A.heads;
+    const int lane = threadIdx.x % 64;
+    const float *a, *b;
+    float *to, d = 1.0f;
+    if (item < borders) {
+        const int p = (int)(item / A.heads), h = (int)(item % A.heads);
+        const Spans::Border e = A.spans.border(p);
+        if (!e.cuts) return;
+        const int before = A.dir > 0 ? p - 1 : p, after = A.dir > 0 ? p : p - 1;
+        a = A.S + ((long long)before * A.heads + h) * A.size;
+        b = A.U + ((long long)after * A.heads + h) * A.size;
+        const int r = A.dir > 0 ? e.row : e.row - 1;  // the first row after the border
+        const float g = A.gs ? A.g[(long long)r * A.gs + h] : A.g[h];
+        d = expf(g);
+        to = A.cut + item;
+    } else {
+        const long long i = item - borders;
+        if (!A.Sl || i >= (long long)A.n_seqs * A.heads) return;
+        const int s = (int)(i / A.heads);
+        if (A.offsets[s] == A.offsets[s + 1]) return;
+        a = A.Sl + i * A.size, b = A.Ul + i * A.size;
+        to = A.last + i;
+    }
+    float z = 0.0f;
+    for (int e = 4 * lane; e < A.size; e += 256) {
+        const o_f32x4 x = *(const o_f32x4 *)(a + e), y = *(const o_f32x4 *)(b + e);
+        z += (x[0] * y[0] + x[1] * y[1]) + (x[2] * y[2] + x[3] * y[3]);
+    }
+    z = wave_sum(z);
+    if (lane == 0) *to = z == 0.0f ? 0.0f : z * d;
+}
+
+// The decays' gradient of a span and head: sums from the span's last row (in the recurrence's order) to
+// its first, sequence by sequence.  The sums are fp64, so that rows far from the end lose nothing.
+__global__ __launch_bounds__(64) void tf_decay_grad_kernel(DecayGrad A) {
+    const int p = blockIdx.x / A.heads, h = blockIdx.x % A.heads, i = threadIdx.x, dir = -A.dir;
+    if (*A.bad) {
+        const float nan = __builtin_nanf("");
+        const long long lo = (long long)p * A.spans.span;
+        const long long hi = lo + A.spans.span < A.spans.n_rows ? lo + A.spans.span : A.spans.n_rows;
+        if (A.gs)
+            for (long long r = lo + i; r < hi; r += 64) A.dg[r * A.heads + h] = nan;
+        else if (i == 0) A.part[(long long)p * A.heads + h] = nan;
+        return;
+    }
+    const Spans::Border b0 = A.spans.border(p), b1 = A.spans.border(p + 1);
+    const int len = b1.row - b0.row, row_first = dir > 0 ? b0.row : b1.row - 1;
+    double carry = 0.0, sum = 0.0;
+    if (dir > 0 ? b0.cuts : b1.cuts) carry = (double)A.cut[(long long)(dir > 0 ? p : p + 1) * A.heads + h];
+    for (int c = 0; c < len; c += 64) {
+        const int row0 = row_first + dir * c, r = row0 + dir * i;
+        const int2 s = c + i < len ? A.spans.info[r] : int2{-1, -1};
+        const bool live = s.x >= 0;
+        int f = i;
+        double v = 0.0;
+        if (live) {
+            f = dir > 0 ? s.x - row0 : row0 - (s.y - 1);
+            v = (double)A.da[(long long)r * A.heads + h] - (double)A.db[(long long)r * A.heads + h];
+            if (f == i && A.last) v += (double)A.last[(long long)seq_of_row(A.offsets, A.n_seqs, r) * A.heads + h];
+        }
+        const int from = f > 0 ? f : 0;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const double o = __shfl_up(v, d);
+            if (i - d >= from) v += o;
+        }
+        if (f < 0) v += carry;
+        carry = __shfl(v, 63);  // (the rows of a chunk before the last are 64)
+        if (live) {
+            const float g = A.gs ? A.g[(long long)r * A.gs + h] : A.g[h];
+            if (g < -104.0f) v = 0.0;  // exp(g) is 0, and so is what it is multiplied with
+            if (A.gs) A.dg[(long long)r * A.heads + h] = (float)v;
+            else sum += v;
+        }
+    }
+    if (!A.gs) {
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+        if (i == 0) A.part[(long long)p * A.heads + h] = (float)sum;
+    }
+}
+
+__global__ __launch_bounds__(64) void tf_decay_sum_kernel(const float *__restrict__ part, int n, int heads, float *__restrict__ dg) {
+    double v = 0.0;
+    for (int p = threadIdx.x; p < n; p += 64) v += (double)part[(long long)p * heads + blockIdx.x];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+    if (threadIdx.x == 0) dg[blockIdx.x] = (float)v;
+}
+
+// Gradients of queries and keys that several heads share: the heads' own, added in order.
+template <class T>
+__global__ __launch_bounds__(256) void tf_decay_share_kernel(const float *__restrict__ part, int group, int shared, int width,
+                                                             long long n_rows, const int32_t *__restrict__ offsets, int n_seqs,
+                                                             typename T::E *__restrict__ out, long long stride, const int *bad) {
+    const int per = shared * width / 4;
+    const long long lo = *bad ? 0 : offsets[0], hi = *bad ? n_rows : offsets[n_seqs];
+    for (long long i = lo * per + (long long)blockIdx.x * 256 + threadIdx.x; i < hi * per; i += (long long)gridDim.x * 256) {
+        const long long r = i / per;
+        const int c = (int)(i - r * per) * 4, hk = c / width, d = c - hk * width;
+        const float *p = part + (r * shared + hk) * (long long)group * width + d;
+        o_f32x4 v = *(const o_f32x4 *)p;
+        for (int j = 1; j < group; ++j) v += *(const o_f32x4 *)(p + (long long)j * width);
+        store4<T>(out + r * stride + c, v);
+    }
+}
+
+// One token of every sequence: the state is read, decayed, added to, multiplied with q and written in one
+// pass.  A workgroup of 256 threads has one head's state; a thread four neighbouring columns of every
+// 256 / (dv / 4)-th row.
+template <class T>
+__global__ __launch_bounds__(256) void tf_decay_step_kernel(const void *__restrict__ q_, long long qs, const void *__restrict__ k_,
+                                                            long long ks, const void *__restrict__ v_, long long vs,
+                                                            const float *__restrict__ g, long long gs, int heads, int group,
+                                                            int dk, int dv, float scale, const float *s0, float *s1, void *out,
+                                                            long long os) {
+    typedef typename T::E E;
+    __shared__ float qk[2][128];
+    __shared__ o_f32x4 sums[256];
+    const long long item = blockIdx.x;
+    const long long i = item / heads;
+    const int h = (int)(item % heads), tid = threadIdx.x, hk = h / group;
+    if (tid < 2 * dk) {
+        const int w = tid >= dk, d = w ? tid - dk : tid;
+        qk[w][d] = w ? (float)((const E *)k_)[i * ks + hk * dk + d] : (float)((const E *)q_)[i * qs + hk * dk + d];
+    }
+    const int cols = dv / 4, rows = 256 / cols, col = tid % cols, row = tid / cols;
+    const float decay = expf(gs ? g[i * gs + h] : g[h]);
+    const E *vp = (const E *)v_ + i * vs + (long long)h * dv + 4 * col;
+    const o_f32x4 v = {(float)vp[0], (float)vp[1], (float)vp[2], (float)vp[3]};
+    const float *s = s0 + item * dk * dv;
+    float *t = s1 + item * dk * dv;
+    __syncthreads();
+    o_f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int d = row; d < dk; d += rows) {
+        o_f32x4 x = *(const o_f32x4 *)(s + d * dv + 4 * col);
+        x = x * decay + v * qk[1][d];
+        *(o_f32x4 *)(t + d * dv + 4 * col) = x;
+        o += x * qk[0][d];
+    }
+    sums[tid] = o;
+    __syncthreads();
+    if (tid < cols) {
+        for (int r = 1; r < rows; ++r) o += sums[r * cols + tid];
+        store4<T>((E *)out + i * os + (long long)h * dv + 4 * tid, o * scale);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------
+
+tf_status decay_check(const tf_decay_config *c) {
+    if (!c || !elem_ok(c->elem) || c->n_heads < 1 || c->n_qk_heads < 1 || c->n_heads % c->n_qk_heads || c->d_k < 1 || c->d_v < 1)
+        return TF_EINVAL;
+    if (!std::isfinite(c->scale) || (c->reverse != 0 && c->reverse != 1)) return TF_EINVAL;
+    auto width = [](int d) { return d == 32 || d == 64 || d == 128; };
+    if (!width(c->d_k) || !width(c->d_v) || c->n_heads > 1024) return TF_EUNSUPPORTED;
+    return TF_OK;
+}
+
+// Rows of a span.  Enough spans that four workgroups fit each compute unit, and no more than that: every
+// border that cuts a sequence costs a state written and read.
+int decay_span(const tf_decay_config *c, int64_t n_rows) {
+    int64_t s = n_rows * c->n_heads / 1024 / kChunk * kChunk;
+    if (s < kMinSpan) s = kMinSpan;
+    if (s > 512) s = 512;
+    return (int)s;
+}
+int64_t decay_spans(const tf_decay_config *c, int64_t n_rows) {
+    const int64_t s = decay_span(c, n_rows), n = (n_rows + s - 1) / s;
+    return n < 1 ? 1 : n;
+}
+
+struct Room {  // parts of the workspace, each at a multiple of 256 bytes
+    char *base;
+    size_t used = 0;
+    explicit Room(void *b) : base((char *)b) {}
+    template <class V> V *take(int64_t n) {
+        V *p = (V *)(base + used);
+        used += ((size_t)n * sizeof(V) + 255) / 256 * 256;
+        return p;
+    }
+};
+struct Plan {
+    int2 *info;
+    int *bad, *kind[2];
+    float *local[2], *mult[2];
+    float *da, *db, *cut, *last, *sl, *part, *dq, *dk;
+    size_t bytes;
+};
+Plan decay_plan(const tf_decay_config *c, int64_t n_rows, int64_t n_seqs, bool back, bool states, void *base) {
+    Room r(base);
+    Plan p = {};
+    const int64_t spans = decay_spans(c, n_rows), h = c->n_heads, size = (int64_t)c->d_k * c->d_v;
+    p.bad = r.take<int>(1);
+    p.info = r.take<int2>(n_rows);
+    for (int i = 0; i < (back ? 2 : 1); ++i) {
+        p.kind[i] = r.take<int>(spans);
+        p.mult[i] = r.take<float>(spans * h);
+        p.local[i] = r.take<float>(spans > 1 ? spans * h * size : 0);
+    }
+    if (back) {
+        p.da = r.take<float>(n_rows * h);
+        p.db = r.take<float>(n_rows * h);
+        p.cut = r.take<float>(spans * h);
+        p.part = r.take<float>(spans * h);
+        if (states) {
+            p.last = r.take<float>(n_seqs * h);
+            p.sl = r.take<float>(n_seqs * h * size);
+        }
+        if (c->n_heads != c->n_qk_heads) {
+            p.dq = r.take<float>(n_rows * h * c->d_k);
+            p.dk = r.take<float>(n_rows * h * c->d_k);
+        }
+    }
+    p.bytes = r.used;
+    return p;
+}
+
+template <class T, int DK, int DV> void span_mode(const DecayRun &A, int mode, hipStream_t s) {
+    const dim3 grid((unsigned)(A.spans.n * A.heads)), block(4 * DV);
+    switch (mode) {
+        case DECAY_STATE: hipLaunchKernelGGL((tf_decay_span_kernel<T, DK, DV, DECAY_STATE>), grid, block, 0, s, A); break;
+        case DECAY_OUT: hipLaunchKernelGGL((tf_decay_span_kernel<T, DK, DV, DECAY_OUT>), grid, block, 0, s, A); break;
+        case DECAY_DOT: hipLaunchKernelGGL((tf_decay_span_kernel<T, DK, DV, DECAY_DOT>), grid, block, 0, s, A); break;
+        default: hipLaunchKernelGGL((tf_decay_span_kernel<T, DK, DV, DECAY_PAIRS>), grid, block, 0, s, A); break;
+    }
+}
+template <class T, int DK> void span_dv(const DecayRun &A, int dv, int mode, hipStream_t s) {
+    if (dv == 32) span_mode<T, DK, 32>(A, mode, s);
+    else if (dv == 64) span_mode<T, DK, 64>(A, mode, s);
+    else span_mode<T, DK, 128>(A, mode, s);
+}
+template <class T> void span_dk(const DecayRun &A, int dk, int dv, int mode, hipStream_t s) {
+    if (dk == 32) span_dv<T, 32>(A, dv, mode, s);
+    else if (dk == 64) span_dv<T, 64>(A, dv, mode, s);
+    else span_dv<T, 128>(A, dv, mode, s);
+}
+void span_run(int elem, const DecayRun &A, int dk, int dv, int mode, hipStream_t s) {
+    if (elem == TF_ELEM_BF16) span_dk<ElemBF16>(A, dk, dv, mode, s);
+    else if (elem == TF_ELEM_FP32) span_dk<ElemF32>(A, dk, dv, mode, s);
+    else span_dk<ElemF16>(A, dk, dv, mode, s);
+}
+// The states at the spans' ends of a run whose arguments k, v, g, s0 are set.
+void chain_run(int elem, DecayRun A, int dk, int dv, hipStream_t s) {
+    if (A.spans.n < 2) return;
+    A.sf = nullptr;
+    A.turned = 0;
+    span_run(elem, A, dk, dv, DECAY_STATE, s);
+    hipLaunchKernelGGL(tf_decay_chain_kernel, dim3((unsigned)(A.spans.n * A.heads), (unsigned)(dk * dv / 1024)), dim3(256), 0, s,
+                       A.local, A.mult, A.kind, A.spans.n, A.heads, dk * dv, A.dir, A.bad);
+}
+void index_run(const int32_t *offsets, int n_seqs, int64_t n_rows, const Plan &p, int32_t *flags, hipStream_t s) {
+    hipLaunchKernelGGL(tf_decay_index_kernel, dim3((unsigned)(1 + (n_rows + 255) / 256)), dim3(256), 0, s, offsets, n_seqs,
+                       (int)n_rows, p.info, p.bad, flags);
+}
+void empty_run(const int32_t *offsets, int n_seqs, long long size, const float *s0, float *sf, const Plan &p, hipStream_t s) {
+    hipLaunchKernelGGL(tf_decay_empty_kernel, dim3(n_seqs < 1024 ? n_seqs : 1024), dim3(256), 0, s, offsets, n_seqs, size, s0, sf,
+                       p.bad);
+}
+template <class T>
+void share_one(const float *part, const tf_decay_config *c, int64_t n_rows, const int32_t *offsets, int n_seqs, void *out,
+               int64_t stride, const int *bad, hipStream_t s) {
+    const int64_t items = n_rows * c->n_qk_heads * c->d_k / 4, blocks = (items + 255) / 256;
+    hipLaunchKernelGGL((tf_decay_share_kernel<T>), dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, s, part,
+                       c->n_heads / c->n_qk_heads, (int)c->n_qk_heads, (int)c->d_k, (long long)n_rows, offsets, n_seqs,
+                       (typename T::E *)out, (long long)stride, bad);
+}
+void share_run(const float *part, const tf_decay_config *c, int64_t n_rows, const int32_t *offsets, int n_seqs, void *out,
+               int64_t stride, const int *bad, hipStream_t s) {
+    if (c->elem == TF_ELEM_BF16) share_one<ElemBF16>(part, c, n_rows, offsets, n_seqs, out, stride, bad, s);
+    else if (c->elem == TF_ELEM_FP32) share_one<ElemF32>(part, c, n_rows, offsets, n_seqs, out, stride, bad, s);
+    else share_one<ElemF16>(part, c, n_rows, offsets, n_seqs, out, stride, bad, s);
+}
+
+bool decay_sizes_ok(const tf_decay_config *c, int64_t n_rows, int32_t n_seqs) {
+    // rows are 32-bit numbers, and so are workgroups
+    return n_rows <= INT32_MAX - 2 * kChunk && decay_spans(c, n_rows) * c->n_heads < INT32_MAX;
+}
+
+}  // namespace
+
+extern "C" size_t tf_decay_workspace_size(const tf_decay_config *c, int64_t n_rows) {
+    if (decay_check(c) != TF_OK || n_rows < 0 || !decay_sizes_ok(c, n_rows, 0)) return 0;
+    return decay_plan(c, n_rows, 0, false, false, nullptr).bytes;
+}
+
+extern "C" size_t tf_decay_backward_workspace_size(const tf_decay_config *c, int64_t n_rows, int32_t n_seqs, int32_t with_d_state) {
+    if (decay_check(c) != TF_OK || n_rows < 0 || n_seqs < 0 || !decay_sizes_ok(c, n_rows, n_seqs)) return 0;
+    return decay_plan(c, n_rows, n_seqs, true, with_d_state != 0, nullptr).bytes;
+}
+
+extern "C" tf_status tf_decay_attention(const tf_decay_config *c, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                                        const void *v, int64_t v_stride, const float *log_decay, int64_t decay_stride,
+                                        int64_t n_rows, const int32_t *offsets, int32_t n_seqs, const float *initial_state,
+                                        void *workspace, size_t workspace_bytes, void *out, int64_t out_stride,
+                                        float *final_state, int32_t *flags, hipStream_t stream) {
+    const tf_status st = decay_check(c);
+    if (st != TF_OK) return st;
+    const int64_t qw = (int64_t)c->n_qk_heads * c->d_k, vw = (int64_t)c->n_heads * c->d_v;
+    if (n_rows < 0 || n_seqs < 0 || (decay_stride != 0 && decay_stride < c->n_heads)) return TF_EINVAL;
+    if (!stride_ok(q_stride, qw, c->elem) || !stride_ok(k_stride, qw, c->elem) || !stride_ok(v_stride, vw, c->elem) ||
+        !stride_ok(out_stride, vw, c->elem))
+        return TF_EINVAL;
+    if (!decay_sizes_ok(c, n_rows, n_seqs)) return TF_EUNSUPPORTED;
+    if (n_seqs == 0) return TF_OK;
+    if (!offsets || !workspace || !log_decay) return TF_EINVAL;
+    if (n_rows > 0 && (!q || !k || !v || !out)) return TF_EINVAL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || ((uintptr_t)workspace & 255)) return TF_EINVAL;
+    const Plan p = decay_plan(c, n_rows, n_seqs, false, false, workspace);
+    if (workspace_bytes < p.bytes) return TF_EINVAL;
+    index_run(offsets, n_seqs, n_rows, p, flags, stream);
+    if (final_state)
+        empty_run(offsets, n_seqs, (long long)c->n_heads * c->d_k * c->d_v, initial_state, final_state, p, stream);
+    if (n_rows > 0) {
+        DecayRun A = {};
+        const int group = c->n_heads / c->n_qk_heads;
+        A.q = q, A.k = k, A.v = v, A.qs = q_stride, A.ks = k_stride, A.vs = v_stride;
+        A.qg = A.kg = group, A.vg = 1, A.xg = 1;
+        A.out = out, A.os = out_stride;
+        A.g = log_decay, A.gs = decay_stride;
+        A.s0 = initial_state, A.sf = final_state;
+        A.local = p.local[0], A.mult = p.mult[0], A.kind = p.kind[0];
+        A.out_scale = c->scale, A.kv_scale = 1.0f;
+        A.offsets = offsets, A.n_seqs = n_seqs, A.heads = c->n_heads, A.dir = c->reverse ? -1 : 1, A.bad = p.bad;
+        A.spans = {p.info, (int)n_rows, decay_span(c, n_rows), (int)decay_spans(c, n_rows)};
+        chain_run(c->elem, A, c->d_k, c->d_v, stream);
+        span_run(c->elem, A, c->d_k, c->d_v, DECAY_OUT, stream);
+    }
+    return hipGetLastError() == hipSuccess ? TF_OK : TF_EHIP;
+}
+
+extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const void *d_out, int64_t d_out_stride, const void *q,
+                                                 int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                                                 int64_t v_stride, const float *log_decay, int64_t decay_stride, int64_t n_rows,
+                                                 const int32_t *offsets, int32_t n_seqs, const float *initial_state,
+                                                 const float *d_state, void *workspace, size_t workspace_bytes, void *dq,
+                                                 int64_t dq_stride, void *dk, int64_t dk_stride, void *dv, int64_t dv_stride,
+                                                 float *d_log_decay, float *d_initial, int32_t *flags, hipStream_t stream) {
+    const tf_status st = decay_check(c);
+    if (st != TF_OK) return st;
+    const int64_t qw = (int64_t)c->n_qk_heads * c->d_k, vw = (int64_t)c->n_heads * c->d_v;
+    if (n_rows < 0 || n_seqs < 0 || (decay_stride != 0 && decay_stride < c->n_heads)) return TF_EINVAL;
+    if (!stride_ok(q_stride, qw, c->elem) || !stride_ok(k_stride, qw, c->elem) || !stride_ok(v_stride, vw, c->elem) ||
+        !stride_ok(d_out_stride, vw, c->elem) || !stride_ok(dq_stride, qw, c->elem) || !stride_ok(dk_stride, qw, c->elem) ||
+        !stride_ok(dv_stride, vw, c->elem))
+        return TF_EINVAL;
+    if (!decay_sizes_ok(c, n_rows, n_seqs)) return TF_EUNSUPPORTED;
+    if (!offsets || !workspace || !log_decay || !d_log_decay) return TF_EINVAL;
+    if (n_rows > 0 && (!q || !k || !v || !d_out || !dq || !dk || !dv)) return TF_EINVAL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(d_out) || !aligned16(dq) || !aligned16(dk) ||
+        !aligned16(dv) || ((uintptr_t)workspace & 255))
+        return TF_EINVAL;
+    const Plan p = decay_plan(c, n_rows, n_seqs, true, d_state != nullptr, workspace);
+    if (workspace_bytes < p.bytes) return TF_EINVAL;
+    const int H = c->n_heads, group = H / c->n_qk_heads, dir = c->reverse ? -1 : 1, size = c->d_k * c->d_v;
+    const long long states = (long long)H * size;
+    index_run(offsets, n_seqs, n_rows, p, flags, stream);
+    if (n_seqs > 0 && d_initial) empty_run(offsets, n_seqs, states, d_state, d_initial, p, stream);
+    DecayRun A = {};
+    A.g = log_decay, A.gs = decay_stride;
+    A.offsets = offsets, A.n_seqs = n_seqs, A.heads = H, A.bad = p.bad;
+    A.spans = {p.info, (int)n_rows, decay_span(c, n_rows), (int)decay_spans(c, n_rows)};
+    if (n_rows > 0 && n_seqs > 0) {
+        // the states at the spans' ends, and their gradients
+        DecayRun F = A;
+        F.k = k, F.ks = k_stride, F.kg = group, F.v = v, F.vs = v_stride, F.vg = 1, F.qg = F.xg = 1;
+        F.s0 = initial_state, F.dir = dir, F.out_scale = F.kv_scale = 1.0f;
+        F.local = p.local[0], F.mult = p.mult[0], F.kind = p.kind[0];
+        chain_run(c->elem, F, c->d_k, c->d_v, stream);
+        DecayRun B = A;
+        B.k = q, B.ks = q_stride, B.kg = group, B.v = d_out, B.vs = d_out_stride, B.vg = 1, B.qg = B.xg = 1;
+        B.s0 = d_state, B.dir = -dir, B.shift = 1, B.out_scale = 1.0f, B.kv_scale = c->scale;
+        B.local = p.local[1], B.mult = p.mult[1], B.kind = p.kind[1];
+        chain_run(c->elem, B, c->d_k, c->d_v, stream);
+        const bool shared = group > 1;
+        // dq
+        DecayRun Q = F;
+        Q.q = d_out, Q.qs = d_out_stride, Q.qg = 1;
+        Q.k = v, Q.ks = v_stride, Q.kg = 1;
+        Q.v = k, Q.vs = k_stride, Q.vg = group;
+        Q.x = q, Q.xs = q_stride, Q.xg = group;
+        Q.out = shared ? (void *)p.dq : dq, Q.os = shared ? (int64_t)H * c->d_k : dq_stride, Q.out_f32 = shared;
+        Q.turned = 1, Q.sf = p.sl, Q.db = p.da, Q.out_scale = c->scale, Q.kv_scale = 1.0f;
+        span_run(c->elem, Q, c->d_v, c->d_k, DECAY_PAIRS, stream);
+        // dk
+        DecayRun K = B;
+        K.q = v, K.qs = v_stride, K.qg = 1;
+        K.k = d_out, K.ks = d_out_stride, K.kg = 1;
+        K.v = q, K.vs = q_stride, K.vg = group;
+        K.x = k, K.xs = k_stride, K.xg = group;
+        K.out = shared ? (void *)p.dk : dk, K.os = shared ? (int64_t)H * c->d_k : dk_stride, K.out_f32 = shared;
+        K.turned = 1, K.db = p.db;
+        span_run(c->elem, K, c->d_v, c->d_k, DECAY_DOT, stream);
+        // dv, and the initial states' gradients
+        DecayRun V = B;
+        V.q = k, V.qs = k_stride, V.qg = group;
+        V.out = dv, V.os = dv_stride;
+        V.sf = d_initial, V.sf_decay = 1;
+        span_run(c->elem, V, c->d_k, c->d_v, DECAY_OUT, stream);
+        if (shared) {
+            share_run(p.dq, c, n_rows, offsets, n_seqs, dq, dq_stride, p.bad, stream);
+            share_run(p.dk, c, n_rows, offsets, n_seqs, dk, dk_stride, p.bad, stream);
+        }
+    }
+    DecayGrad G = {};
+    G.spans = A.spans, G.S = p.local[0], G.U = p.local[1], G.Sl = p.sl, G.Ul = d_state, G.cut = p.cut, G.last = p.last;
+    G.g = log_decay, G.gs = decay_stride, G.da = p.da, G.db = p.db, G.dg = d_log_decay, G.part = p.part;
+    G.offsets = offsets, G.n_seqs = n_seqs, G.heads = H, G.dir = dir, G.size = size, G.bad = p.bad;
+    if (n_rows > 0 && n_seqs > 0) {
+        const long long items = (long long)G.spans.n * H + (d_state ? (long long)n_seqs * H : 0);
+        if (G.spans.n > 1 || d_state)
+            hipLaunchKernelGGL(tf_decay_dots_kernel, dim3((unsigned)((items + 3) / 4)), dim3(256), 0, stream, G);
+    }
+    if (n_rows > 0 || !decay_stride)
+        hipLaunchKernelGGL(tf_decay_grad_kernel, dim3((unsigned)(G.spans.n * H)), dim3(64), 0, stream, G);
+    if (!decay_stride)
+        hipLaunchKernelGGL(tf_decay_sum_kernel, dim3(H), dim3(64), 0, stream, p.part, G.spans.n, H, d_log_decay);
+    return hipGetLastError() == hipSuccess ? TF_OK : TF_EHIP;
+}
+
+extern "C" tf_status tf_decay_attention_step(const tf_decay_config *c, const void *q, int64_t q_stride, const void *k,
+                                             int64_t k_stride, const void *v, int64_t v_stride, const float *log_decay,
+                                             int64_t decay_stride, int32_t n_seqs, const float *state, float *state_out, void *out,
+                                             int64_t out_stride, hipStream_t stream) {
+    const tf_status st = decay_check(c);
+    if (st != TF_OK) return st;
+    const int64_t qw = (int64_t)c->n_qk_heads * c->d_k, vw = (int64_t)c->n_heads * c->d_v;
+    if (n_seqs < 0 || (decay_stride != 0 && decay_stride < c->n_heads)) return TF_EINVAL;
+    if (!stride_ok(q_stride, qw, c->elem) || !stride_ok(k_stride, qw, c->elem) || !stride_ok(v_stride, vw, c->elem) ||
+        !stride_ok(out_stride, vw, c->elem))
+        return TF_EINVAL;
+    if ((int64_t)n_seqs * c->n_heads > INT32_MAX) return TF_EUNSUPPORTED;
+    if (n_seqs == 0) return TF_OK;
+    if (!q || !k || !v || !log_decay || !state || !state_out || !out) return TF_EINVAL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(state) || !aligned16(state_out))
+        return TF_EINVAL;
+    const dim3 grid((unsigned)((int64_t)n_seqs * c->n_heads));
+    const int group = c->n_heads / c->n_qk_heads;
+#define TF_STEP(T)                                                                                                               \
+    hipLaunchKernelGGL((tf_decay_step_kernel<T>), grid, dim3(256), 0, stream, q, (long long)q_stride, k, (long long)k_stride, v, \
+                       (long long)v_stride, log_decay, (long long)decay_stride, (int)c->n_heads, group, (int)c->d_k,             \
+                       (int)c->d_v, c->scale, state, state_out, out, (long long)out_stride)
+    if (c->elem == TF_ELEM_BF16) TF_STEP(ElemBF16);
+    else if (c->elem == TF_ELEM_FP32) TF_STEP(ElemF32);
+    else TF_STEP(ElemF16);
+#undef TF_STEP
+    return hipGetLastError() == hipSuccess ? TF_OK : TF_EHIP;
+}

@@ -1,0 +1,65 @@
+// Building blocks of the sequence-layer operators (qknorm.hip, decay.hip,
+// gated.hip): the tensors' element types, their vector loads and stores, and
+// the sequence of a packed row.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "trackfit.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(2))) unsigned int o_u32x2;
+typedef __attribute__((ext_vector_type(4))) unsigned int o_u32x4;
+typedef __attribute__((ext_vector_type(4))) float o_f32x4;
+typedef __attribute__((ext_vector_type(8))) float o_f32x8;
+
+// 8 consecutive elements as one or two 16-byte accesses; E is the element
+// type, V8 a vector of 8 of them.
+struct ElemF32 {
+    typedef float E;
+    typedef o_f32x8 V8;
+};
+struct ElemBF16 {
+    typedef __bf16 E;
+    typedef __attribute__((ext_vector_type(8))) __bf16 V8;
+};
+struct ElemF16 {
+    typedef _Float16 E;
+    typedef __attribute__((ext_vector_type(8))) _Float16 V8;
+};
+
+template <typename T> __device__ __forceinline__ o_f32x8 load8(const typename T::E *p) {
+    return __builtin_convertvector(*(const typename T::V8 *)p, o_f32x8);
+}
+// Round to nearest even to the element type: the one rounding of an output.
+template <typename T> __device__ __forceinline__ void store8(typename T::E *p, o_f32x8 v) {
+    *(typename T::V8 *)p = __builtin_convertvector(v, typename T::V8);
+}
+
+// The sequence that packed row r belongs to: the last i < n with offsets[i] <= r (so that
+// empty sequences own no row), or -1 when there is none or r is at or past its end.
+// Any offsets: the search stays inside [0, n].
+__device__ __forceinline__ int seq_of_row(const int32_t *__restrict__ offsets, int n, long long r) {
+    int lo = 0, hi = n;  // offsets[lo - 1] <= r < offsets[hi], where these exist
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (offsets[mid] <= r) lo = mid + 1;
+        else hi = mid;
+    }
+    if (lo == 0 || r >= offsets[lo]) return -1;  // lo <= n: offsets has n + 1 entries
+    return lo - 1;
+}
+
+inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+inline size_t elem_bytes(int e) { return e == TF_ELEM_FP32 ? 4 : 2; }
+inline bool elem_ok(int e) { return e == TF_ELEM_FP32 || e == TF_ELEM_BF16 || e == TF_ELEM_FP16; }
+// A row stride in elements that keeps 16-byte accesses of an aligned array aligned.
+inline bool stride_ok(int64_t stride, int64_t width, int e) {
+    return stride >= width && (stride * (int64_t)elem_bytes(e)) % 16 == 0;
+}
+
+}  // namespace
