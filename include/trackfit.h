@@ -574,6 +574,42 @@ tf_status tf_qk_norm_rotate_backward(const tf_qk_norm_config *cfg, const void *d
                                      int32_t n_seqs, void *workspace, size_t workspace_bytes, void *dq, int64_t dq_stride,
                                      void *dk, int64_t dk_stride, float *dq_gain, float *dk_gain, hipStream_t stream);
 
+/*
+ * The gated feed-forward block's first half, both projections, the activation and
+ * the product in one kernel: h = act(x W_g^T) * (x W_u^T), x [n_rows][width], weights
+ * [inner][width], h [n_rows][inner].  SiLU a / (1 + exp(-a)), GELU a Phi(a).
+ * Sums in fp32 (fp32 tensors: products by the fp32 matrix instruction); the
+ * activation and the product in fp32, one rounding at the store.
+ * Supported: width a multiple of 8, any inner, both up to 2^20.
+ */
+typedef enum { TF_ACT_SILU = 0, TF_ACT_GELU = 1 } tf_activation;
+
+typedef struct {
+    int32_t elem;        /* tf_elem of all tensors */
+    int32_t width;
+    int32_t inner;
+    int32_t activation;  /* tf_activation */
+} tf_gated_config;
+
+/* out's pointer and stride need no alignment beyond the element's; both weights have
+ * w_stride. */
+tf_status tf_gated_ffn(const tf_gated_config *cfg, const void *x, int64_t x_stride, int64_t n_rows, const void *w_gate,
+                       const void *w_up, int64_t w_stride, void *out, int64_t out_stride, hipStream_t stream);
+
+/* Bytes of workspace of the backward pass (0 if invalid). */
+size_t tf_gated_ffn_workspace_size(const tf_gated_config *cfg, int64_t n_rows);
+
+/*
+ * Gradients of x and both weights from that of the output (d_out as out).  The
+ * projections are computed again; their gradients are rounded once to the tensors'
+ * type (they are operands of the products that follow).  Both weights' gradients
+ * have dw_stride; with n_rows 0 they are zeros.
+ */
+tf_status tf_gated_ffn_backward(const tf_gated_config *cfg, const void *d_out, int64_t d_out_stride, const void *x,
+                                int64_t x_stride, int64_t n_rows, const void *w_gate, const void *w_up, int64_t w_stride,
+                                void *workspace, size_t workspace_bytes, void *dx, int64_t dx_stride, void *dw_gate,
+                                void *dw_up, int64_t dw_stride, hipStream_t stream);
+
 /* Static description of a status code (library plumbing: no passage of the
  * paper defines it). */
 const char *tf_status_string(tf_status s);

@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libtrackfit.so")
 SRCS = [os.path.join(HERE, "csrc", f) for f in ("trackfit.hip", "seed.hip", "readout.hip", "mingru.hip", "qknorm.hip",
-                                               "decay.hip")]
+                                               "decay.hip", "gated.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

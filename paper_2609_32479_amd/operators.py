@@ -16,7 +16,8 @@ import math
 import torch
 
 __all__ = ["decay_attention", "decay_attention_backward", "decay_attention_step", "qk_norm_rotate",
-           "qk_norm_rotate_backward", "SEQ_BAD_OFFSETS", "DecayConfig", "QKNormConfig"]
+           "qk_norm_rotate_backward", "gated_ffn", "gated_ffn_backward", "SEQ_BAD_OFFSETS", "DecayConfig", "QKNormConfig",
+           "GatedConfig"]
 
 SEQ_BAD_OFFSETS = 1
 _ELEMS = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -33,14 +34,19 @@ class QKNormConfig(ctypes.Structure):
                 ("interleaved", _i32), ("eps", _f32), ("base", ctypes.c_double)]
 
 
+class GatedConfig(ctypes.Structure):
+    _fields_ = [("elem", _i32), ("width", _i32), ("inner", _i32), ("activation", _i32)]
+
+
 EXPORTED = ("tf_decay_workspace_size", "tf_decay_backward_workspace_size", "tf_decay_attention",
             "tf_decay_attention_backward", "tf_decay_attention_step", "tf_qk_norm_rotate", "tf_qk_norm_workspace_size",
-            "tf_qk_norm_rotate_backward")
+            "tf_qk_norm_rotate_backward", "tf_gated_ffn", "tf_gated_ffn_workspace_size", "tf_gated_ffn_backward")
+_ACTIVATIONS = {"silu": 0, "gelu": 1}
 
 
 def declare(L) -> None:
     """Set the C prototypes on the loaded library."""
-    dc, nc = ctypes.POINTER(DecayConfig), ctypes.POINTER(QKNormConfig)
+    dc, nc, gc = ctypes.POINTER(DecayConfig), ctypes.POINTER(QKNormConfig), ctypes.POINTER(GatedConfig)
     t = [_vp, _i64]  # a tensor and its row stride
     protos = {
         "tf_decay_workspace_size": (_sz, [dc, _i64]),
@@ -53,6 +59,9 @@ def declare(L) -> None:
         "tf_qk_norm_rotate": (ctypes.c_int, [nc, *t, *t, _i64, _vp, _vp, _vp, _vp, _i32, *t, *t, _vp]),
         "tf_qk_norm_rotate_backward": (ctypes.c_int, [nc, *t, *t, *t, *t, _i64, _vp, _vp, _vp, _vp, _i32, _vp, _sz, *t, *t,
                                                       _vp, _vp, _vp]),
+        "tf_gated_ffn": (ctypes.c_int, [gc, *t, _i64, _vp, _vp, _i64, *t, _vp]),
+        "tf_gated_ffn_workspace_size": (_sz, [gc, _i64]),
+        "tf_gated_ffn_backward": (ctypes.c_int, [gc, *t, *t, _i64, _vp, _vp, _i64, _vp, _sz, *t, _vp, _vp, _i64, _vp]),
     }
     for name, (res, args) in protos.items():
         f = getattr(L, name)
@@ -347,3 +356,67 @@ def qk_norm_rotate_backward(dq_out, dk_out, q, k, q_gain, k_gain, offsets=None, 
             q_gain.data_ptr(), k_gain.data_ptr(), _ptr(positions), _ptr(offsets), n, ws.data_ptr(), _bytes(ws),
             dq.data_ptr(), dqs, dk.data_ptr(), dks, dq_gain.data_ptr(), dk_gain.data_ptr(), s), "tf_qk_norm_rotate_backward")
     return dq, dk, dq_gain, dk_gain
+
+
+def _matrix(name: str, x, like: torch.Tensor, rows=None, cols=None) -> int:
+    """Check a [rows, cols] matrix with unit column stride; returns its row stride."""
+    _same(name, x, like, like.dtype)
+    if x.dim() != 2 or (rows is not None and x.shape[0] != rows) or (cols is not None and x.shape[1] != cols):
+        want = ", ".join("?" if v is None else str(v) for v in (rows, cols))
+        raise ValueError(f"{name} must have shape [{want}], not {list(x.shape)}")
+    if x.shape[1] > 1 and x.stride(1) != 1:
+        raise ValueError(f"{name}'s rows must be contiguous")
+    if x.shape[0] <= 1:
+        return x.shape[1]
+    if x.stride(0) < x.shape[1]:
+        raise ValueError(f"{name}'s rows overlap")
+    return x.stride(0)
+
+
+def _gated_inputs(x, w_gate, w_up, activation):
+    elem = _elem(x)
+    if activation not in _ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(_ACTIVATIONS)}")
+    xs = _matrix("x", x, x)
+    ws = _matrix("w_gate", w_gate, x, None, x.shape[1])
+    wu = _matrix("w_up", w_up, x, w_gate.shape[0], x.shape[1])
+    if ws != wu:
+        raise ValueError("w_gate and w_up must have the same row stride")
+    return GatedConfig(elem, x.shape[1], w_gate.shape[0], _ACTIVATIONS[activation]), xs, ws
+
+
+def gated_ffn(x, w_gate, w_up, activation="silu", out=None, stream=None):
+    """act(x w_gate^T) * (x w_up^T) in one kernel: x [rows, width], both weights
+    [inner, width], of one type (fp32, bf16, fp16); activation "silu" or "gelu" (a
+    Phi(a)).  Returns [rows, inner]."""
+    cfg, xs, ws = _gated_inputs(x, w_gate, w_up, activation)
+    with _on(x, stream) as s:
+        if out is None:
+            out = torch.empty((x.shape[0], cfg.inner), dtype=x.dtype, device=x.device)
+        os = _matrix("out", out, x, x.shape[0], cfg.inner)
+        _check(_lib().tf_gated_ffn(ctypes.byref(cfg), x.data_ptr(), xs, x.shape[0], w_gate.data_ptr(), w_up.data_ptr(), ws,
+                                   out.data_ptr(), os, s), "tf_gated_ffn")
+    return out
+
+
+def gated_ffn_backward(d_out, x, w_gate, w_up, activation="silu", dx=None, dw_gate=None, dw_up=None, workspace=None,
+                       stream=None):
+    """Gradients of gated_ffn's inputs: (dx, dw_gate, dw_up).  The projections are
+    computed again from x and the weights."""
+    cfg, xs, ws = _gated_inputs(x, w_gate, w_up, activation)
+    rows = x.shape[0]
+    ds = _matrix("d_out", d_out, x, rows, cfg.inner)
+    with _on(x, stream) as s:
+        dx = torch.empty_like(x, memory_format=torch.contiguous_format) if dx is None else dx
+        dw_gate = torch.empty_like(w_gate, memory_format=torch.contiguous_format) if dw_gate is None else dw_gate
+        dw_up = torch.empty_like(w_up, memory_format=torch.contiguous_format) if dw_up is None else dw_up
+        dxs = _matrix("dx", dx, x, *x.shape)
+        dws = _matrix("dw_gate", dw_gate, x, *w_gate.shape)
+        if _matrix("dw_up", dw_up, x, *w_up.shape) != dws:
+            raise ValueError("dw_gate and dw_up must have the same row stride")
+        wk = _workspace(workspace, int(_lib().tf_gated_ffn_workspace_size(ctypes.byref(cfg), rows)), x)
+        _check(_lib().tf_gated_ffn_backward(
+            ctypes.byref(cfg), d_out.data_ptr(), ds, x.data_ptr(), xs, rows, w_gate.data_ptr(), w_up.data_ptr(), ws,
+            wk.data_ptr(), _bytes(wk), dx.data_ptr(), dxs, dw_gate.data_ptr(), dw_up.data_ptr(), dws, s),
+            "tf_gated_ffn_backward")
+    return dx, dw_gate, dw_up
