@@ -950,8 +950,8 @@ extern "C" tf_status tf_decay_attention(const tf_decay_config *c, const void *q,
         return TF_EINVAL;
     if (!decay_sizes_ok(c, n_rows, n_seqs)) return TF_EUNSUPPORTED;
     if (n_seqs == 0) return TF_OK;
-    if (!offsets || !workspace || !log_decay) return TF_EINVAL;
-    if (n_rows > 0 && (!q || !k || !v || !out)) return TF_EINVAL;
+    if (!offsets || !workspace) return TF_EINVAL;
+    if (n_rows > 0 && (!q || !k || !v || !out || !log_decay)) return TF_EINVAL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || ((uintptr_t)workspace & 255)) return TF_EINVAL;
     const Plan p = decay_plan(c, n_rows, n_seqs, false, false, workspace);
     if (workspace_bytes < p.bytes) return TF_EINVAL;
@@ -992,8 +992,8 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
         !stride_ok(dv_stride, vw, c->elem))
         return TF_EINVAL;
     if (!decay_sizes_ok(c, n_rows, n_seqs)) return TF_EUNSUPPORTED;
-    if (!offsets || !workspace || !log_decay || !d_log_decay) return TF_EINVAL;
-    if (n_rows > 0 && (!q || !k || !v || !d_out || !dq || !dk || !dv)) return TF_EINVAL;
+    if (!offsets || !workspace || (!decay_stride && !d_log_decay)) return TF_EINVAL;
+    if (n_rows > 0 && (!q || !k || !v || !d_out || !dq || !dk || !dv || !log_decay || !d_log_decay)) return TF_EINVAL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(d_out) || !aligned16(dq) || !aligned16(dk) ||
         !aligned16(dv) || ((uintptr_t)workspace & 255))
         return TF_EINVAL;
