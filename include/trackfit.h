@@ -455,7 +455,7 @@ typedef enum { TF_ELEM_FP32 = 0, TF_ELEM_BF16 = 1, TF_ELEM_FP16 = 2 } tf_elem;
  * consecutive heads; values, decays, states and outputs have n_heads.
  * Log decays are meant to be <= 0; below about -104 (-inf too) a row forgets all
  * before it.  reverse = 1: t runs from each sequence's last row to its first.
- * Supported: d_k and d_v 32, 64 or 128, up to 1024 heads.
+ * Supported: d_k and d_v 32, 64 or 128, up to 1024 heads, row strides up to 2^24.
  * fp32 tensors: products and sums in fp32.  bf16: states, decays and sums in fp32;
  * the weights exp(b_t - b_s) q_t k_s of the values inside a chunk of 64 rows are
  * rounded to bf16.  fp16: as fp32, rounded once at the store.

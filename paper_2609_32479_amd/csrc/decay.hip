@@ -41,6 +41,7 @@
 #include "ops.h"
 
 #include <cmath>
+#include <initializer_list>
 
 namespace {
 
@@ -125,6 +126,15 @@ template <class M> constexpr int parts_of(int n) { return M::KM == 32 ? n : 1; }
 template <class T> struct MatOf { typedef MatF32 M; };
 template <> struct MatOf<ElemBF16> { typedef MatBF16 M; };
 
+// Rows of a workgroup of the index; workgroups that check the offsets, each with a word of its own for what it finds.
+constexpr int kIndexRows = 1024, kCheckers = 16;
+__device__ __forceinline__ bool any_bad(const int *__restrict__ bad) {
+    int b = 0;
+#pragma unroll
+    for (int i = 0; i < kCheckers; ++i) b |= bad[i];
+    return b;
+}
+
 // Where the spans' borders are.
 struct Spans {
     const int2 *info;  // first and past-the-last row of each row's sequence, (-1, -1) outside of all
@@ -164,6 +174,7 @@ struct DecayRun {
     float *mult;                         // [spans][heads]: decay over a span that is all one sequence's
     int *kind;                           // [spans]: 0 its end cuts no sequence, 1 it does, 2 and its start cuts the same
     float *db;                           // [n_rows][heads]
+    int pairs;                           // db has the chunks' pairs of rows too
     float out_scale, kv_scale;
     const int32_t *offsets;
     int n_seqs, heads, dir;
@@ -171,60 +182,72 @@ struct DecayRun {
     Spans spans;
 };
 
-enum { DECAY_STATE = 0, DECAY_OUT = 1, DECAY_DOT = 2, DECAY_PAIRS = 3 };
+// A launch's runs: one, or two of the same shapes side by side (blockIdx.y).
+struct DecayRuns {
+    DecayRun run[2];
+};
+
+enum { DECAY_STATE = 0, DECAY_OUT = 1, DECAY_DOT = 2 };
 
 __device__ __forceinline__ float log_decay_of(const DecayRun &A, int r, int h) {
     const float g = A.gs ? A.g[(long long)r * A.gs + h] : A.g[h];
     return g < kForget ? kForget : g;  // (NaN stays)
 }
 
-// The 16-byte pieces of a [64][D] tile that a thread brings from memory to LDS.
+// The 16-byte pieces of a [64][D] tile that a thread brings from memory to LDS.  Rows are counted from the chunk's
+// first in memory: a thread's are p, p + NT / PIECES, ...; in LDS they lie in the recurrence's order.
 template <class T, class M, int D, int NT> struct Tile {
     typedef typename T::E E;
     typedef typename M::E ME;
-    static constexpr int VEC = 16 / sizeof(E), PIECES = D / VEC, ALL = kChunk * PIECES, N = (ALL + NT - 1) / NT;
+    static constexpr int VEC = 16 / sizeof(E), PIECES = D / VEC, STEP = NT / PIECES, N = (kChunk + STEP - 1) / STEP;
     o_u32x4 raw[N];
-    // rows row0 + dir * i, i < rows, inside [lo, hi); zeros for the others
-    __device__ __forceinline__ void load(const void *base, long long stride, int col, int row0, int dir, int rows, int lo,
-                                         int hi, int tid) {
+    __device__ __forceinline__ void load(const void *base, long long stride, int rows, int tid) {
+        const int p = tid / PIECES;
+        const unsigned at = (unsigned)(p * (int)stride + tid % PIECES * VEC) * (unsigned)sizeof(E);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const int c = tid + j * NT, i = c / PIECES, r = row0 + dir * i;
+            const char *b = (const char *)base + (long long)j * STEP * stride * (long long)sizeof(E);
             raw[j] = o_u32x4{0, 0, 0, 0};
-            if (c < ALL && i < rows && r >= lo && r < hi)
-                raw[j] = *(const o_u32x4 *)((const E *)base + (long long)r * stride + col + (c % PIECES) * VEC);
+            if (p + j * STEP < rows) raw[j] = *(const o_u32x4 *)(b + at);
         }
     }
-    __device__ __forceinline__ void store(ME *lds, int tid) const {
+    __device__ __forceinline__ void store(ME *lds, int rows, int dir, int tid) const {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const int c = tid + j * NT;
-            if (ALL % NT && c >= ALL) break;
-            ME *p = lds + (c / PIECES) * (D + M::PAD) + (c % PIECES) * VEC;
+            const int p = tid / PIECES + j * STEP;
+            if (N * STEP > kChunk && p >= kChunk) break;
+            const int i = dir < 0 && p < rows ? rows - 1 - p : p;
+            ME *q = lds + i * (D + M::PAD) + tid % PIECES * VEC;
             if constexpr (sizeof(ME) == sizeof(E)) {
-                *(o_u32x4 *)p = raw[j];
+                *(o_u32x4 *)q = raw[j];
             } else {  // fp16 to fp32
                 typedef __attribute__((ext_vector_type(8))) _Float16 H8;
-                *(o_f32x8 *)p = __builtin_convertvector(__builtin_bit_cast(H8, raw[j]), o_f32x8);
+                *(o_f32x8 *)q = __builtin_convertvector(__builtin_bit_cast(H8, raw[j]), o_f32x8);
             }
         }
     }
-    __device__ __forceinline__ bool infinite() const {  // or NaN
-        unsigned bad = 0;
+    __device__ __forceinline__ bool infinite() const {  // or NaN: the largest exponent there is
+        if constexpr (sizeof(E) == 4) {
+            unsigned most = 0;
 #pragma unroll
-        for (int j = 0; j < N; ++j)
+            for (int j = 0; j < N; ++j)
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const unsigned u = raw[j][w];
-                if constexpr (sizeof(E) == 4) {
-                    bad |= (u & 0x7fffffffu) >= 0x7f800000u;
-                } else {
-                    constexpr unsigned top = sizeof(ME) == 2 ? 0x7f80u : 0x7c00u;
-                    bad |= (u & 0x7fffu) >= top;
-                    bad |= ((u >> 16) & 0x7fffu) >= top;
+                for (int w = 0; w < 4; ++w) {
+                    const unsigned u = raw[j][w] & 0x7fffffffu;
+                    most = most > u ? most : u;
                 }
-            }
-        return bad != 0;
+            return most >= 0x7f800000u;
+        } else {
+            typedef __attribute__((ext_vector_type(2))) unsigned short H2;
+            H2 most = {0, 0};
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    most = __builtin_elementwise_max(most, __builtin_bit_cast(H2, raw[j][w] & 0x7fff7fffu));
+            constexpr unsigned short top = sizeof(ME) == 2 ? 0x7f80 : 0x7c00;
+            return most[0] >= top || most[1] >= top;
+        }
     }
 };
 
@@ -233,16 +256,37 @@ template <class T> __device__ __forceinline__ void store4(typename T::E *p, o_f3
     *(V *)p = __builtin_convertvector(v, V);
 }
 
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+// 2^x of an fp64 x, to fp32's precision
+__device__ __forceinline__ float exp2_of(double x) {
+    const float h = (float)x;
+    const float e = exp2_hw(h), l = (float)(x - (double)h);
+    return l == l ? fmaf(e, l * 0.693147180559945f, e) : e;  // (h infinite: no rest)
+}
+
+// What the products need to know of a chunk's rows, in the recurrence's order.
+struct ChunkRows {
+    float bh[kChunk], bl[kChunk];  // sum of the log2 decays from the chunk's first row, or the sequence's, to the row: high and low part
+    float in[kChunk];              // 2^b times out_scale: what the state before brings to the row
+    float to[kChunk];              // 2^(b_end - b) times kv_scale: what the row brings to the state after
+    float decay[kChunk];           // 2^b
+    int seg[kChunk];               // the sequence: its first row in the chunk + 1 (0: before the chunk), its last + 1 << 8, 1 << 16 if it ends there
+};
+__device__ __forceinline__ int seg_first(int s) { return (s & 255) - 1; }
+__device__ __forceinline__ int seg_past(int s) { return (s >> 8) & 255; }
+__device__ __forceinline__ bool seg_ends(int s) { return s >> 16; }
+
 // One span of one head.  Waves: each owns 16 of the state's and the output's columns; the state
 // stays in its accumulators over the span.  The 64 x 64 weights of a chunk are computed once,
-// 16 x 16 tiles on or below the diagonal dealt out to the waves, and pass through LDS.
+// 16 x 16 tiles on or below the diagonal dealt out to the waves, and pass through LDS.  The next chunk's rows of
+// the tensors are on their way to registers meanwhile, and its row sums are one wave's work beside the products.
 template <class T, int DK, int DV, int MODE>
-__global__ __launch_bounds__(4 * DV) void tf_decay_span_kernel(DecayRun A) {
+__global__ __launch_bounds__(4 * DV, DK * DV <= 64 * 64 && DV == 64 ? 3 : 2) void tf_decay_span_kernel(DecayRuns R) {
     typedef typename MatOf<T>::M M;
     typedef typename M::E ME;
     typedef typename M::F F;
-    constexpr bool OUT = MODE >= DECAY_OUT, DOT = MODE >= DECAY_DOT, PAIRS = MODE == DECAY_PAIRS;
-    constexpr int NW = DV / 16, NT = 64 * NW, KM = M::KM;
+    constexpr bool OUT = MODE >= DECAY_OUT, DOT = MODE >= DECAY_DOT;
+    constexpr int NW = DV / 16, NT = 64 * NW, KM = M::KM, ES = sizeof(typename T::E);
     constexpr int LK = DK + M::PAD, LV = DV + M::PAD, LP = kChunk + M::PAD;
     constexpr int ST = DK / 16;                    // state tiles of a wave
     constexpr int NB = kChunk / KM;                // fragments along a chunk's rows
@@ -250,14 +294,17 @@ __global__ __launch_bounds__(4 * DV) void tf_decay_span_kernel(DecayRun A) {
     constexpr int NU = parts_of<M>(3);             // parts of the weighted v in the state's update
     __shared__ __attribute__((aligned(16))) ME Qs[OUT ? kChunk * LK : 8], Ks[kChunk * LK], Vs[kChunk * LV],
         Xs[DOT ? kChunk * LV : 8], Ps[OUT ? kChunk * LP : 8];
-    __shared__ float bh[kChunk], bl[kChunk], fo[kChunk], wt[kChunk], endd[kChunk];
-    __shared__ int first[kChunk], past[kChunk], stat[kChunk];
-    __shared__ float rowp[PAIRS ? 4 : 1][kChunk], colp[PAIRS ? 4 : 1][kChunk], dots[DOT ? NW : 1][kChunk];
+    __shared__ ChunkRows rows_of[2];
+    __shared__ float rowp[DOT ? 4 : 1][kChunk], colp[DOT ? 4 : 1][kChunk], dots[DOT ? NW : 1][kChunk];
 
+    const DecayRun &A = R.run[blockIdx.y];
+    const bool pairs = MODE == DECAY_DOT && A.pairs;
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int n = lane % 16, q = lane / 16, c0 = 16 * wave;
     const int p = blockIdx.x / A.heads, h = blockIdx.x % A.heads, dir = A.dir;
-    if (*A.bad) {
+    const int bad = any_bad(A.bad), olo = A.offsets[0], ohi = A.offsets[A.n_seqs];
+    const Spans::Border b0 = A.spans.border(p), b1 = A.spans.border(p + 1);
+    if (bad) {
         if (OUT) {  // offsets that make no sequences: every row of the array is NaN
             const long long lo = (long long)p * A.spans.span;
             const long long hi = lo + A.spans.span < A.spans.n_rows ? lo + A.spans.span : A.spans.n_rows;
@@ -270,7 +317,6 @@ __global__ __launch_bounds__(4 * DV) void tf_decay_span_kernel(DecayRun A) {
         }
         return;
     }
-    const Spans::Border b0 = A.spans.border(p), b1 = A.spans.border(p + 1);
     int lo = b0.row, hi = b1.row;
     const bool cut_in = dir > 0 ? b0.cuts : b1.cuts, cut_out = dir > 0 ? b1.cuts : b0.cuts;
     bool whole = false;
@@ -286,131 +332,147 @@ __global__ __launch_bounds__(4 * DV) void tf_decay_span_kernel(DecayRun A) {
         }
         if (h == 0 && tid == 0) A.kind[p] = kind;
         if (!cut_out) return;
+    } else {
+        // rows outside of all sequences are before the first and behind the last
+        lo = lo > olo ? lo : olo;
+        hi = hi < ohi ? hi : ohi;
     }
     if (hi <= lo) return;
     // Chunks are counted from the span's first row in memory whichever way they are run through, so that the runs of
     // both directions have the same ones (db's two halves are split by chunks).
     const int chunks = (hi - lo + kChunk - 1) / kChunk;
-    const int olo = A.offsets[0], ohi = A.offsets[A.n_seqs];
 
     o_f32x4 S[ST];
 #pragma unroll
     for (int m = 0; m < ST; ++m) S[m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
     bool have = false;  // the state is that of the sequence that goes on
     auto load_state = [&](const float *s) {
+        const int step = A.turned ? 1 : DV;
+        const float *e = s + (A.turned ? (c0 + n) * DK + 4 * q : 4 * q * DV + c0 + n);
 #pragma unroll
         for (int m = 0; m < ST; ++m)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int a = 16 * m + 4 * q + i, b = c0 + n;
-                S[m][i] = A.turned ? s[b * DK + a] : s[a * DV + b];
-            }
+            for (int i = 0; i < 4; ++i) S[m][i] = e[(16 * m + i) * step];
     };
     if (OUT && cut_in) {
         load_state(A.local + ((long long)(p - dir) * A.heads + h) * (DK * DV));
         have = true;
     }
-    if (OUT) {  // the weights above the diagonal that share a fragment with some below
-        for (int i = tid; i < kChunk * LP; i += NT) Ps[i] = (ME)0.0f;
-    }
 
     Tile<T, M, DK, NT> tq, tk;
     Tile<T, M, DV, NT> tv, tx;
-    const int hq = h / A.qg * DK, hk = h / A.kg * DK, hv = h / A.vg * DV, hx = DOT ? h / A.xg * DV : 0;
-    auto chunk_at = [&](int c, int &row0, int &rows) {  // the c-th chunk on the way: its first row on the way, its rows
-        const int at = lo + (dir > 0 ? c : chunks - 1 - c) * kChunk;
-        rows = hi - at < kChunk ? hi - at : kChunk;
-        row0 = dir > 0 ? at : at + rows - 1;
-    };
+    // the head's columns, at the span's first row
+    const char *bq = nullptr, *bx = nullptr;
+    if (OUT) bq = (const char *)A.q + ((long long)lo * A.qs + h / A.qg * DK) * ES;
+    const char *bk = (const char *)A.k + ((long long)lo * A.ks + h / A.kg * DK) * ES;
+    const char *bv = (const char *)A.v + ((long long)lo * A.vs + h / A.vg * DV) * ES;
+    if (DOT) bx = (const char *)A.x + ((long long)lo * A.xs + h / A.xg * DV) * ES;
+    auto chunk_rows = [&](int at) { return hi - lo - at < kChunk ? hi - lo - at : kChunk; };
+    auto chunk_at = [&](int c) { return (dir > 0 ? c : chunks - 1 - c) * kChunk; };  // the c-th on the way: its first row in memory, from lo
     auto fetch = [&](int c) {
-        int row0, rows;
-        chunk_at(c, row0, rows);
-        if (OUT) tq.load(A.q, A.qs, hq, row0, dir, rows, olo, ohi, tid);
-        tk.load(A.k, A.ks, hk, row0, dir, rows, olo, ohi, tid);
-        tv.load(A.v, A.vs, hv, row0, dir, rows, olo, ohi, tid);
-        if (DOT) tx.load(A.x, A.xs, hx, row0, dir, rows, olo, ohi, tid);
+        const int at = chunk_at(c), rows = chunk_rows(at);
+        if (OUT) tq.load(bq + (long long)at * A.qs * ES, A.qs, rows, tid);
+        tk.load(bk + (long long)at * A.ks * ES, A.ks, rows, tid);
+        tv.load(bv + (long long)at * A.vs * ES, A.vs, rows, tid);
+        if (DOT) tx.load(bx + (long long)at * A.xs * ES, A.xs, rows, tid);
+    };
+    // The last wave's: a chunk's sequences and decays, one row a lane.
+    int2 next_seq = {0, 0};
+    float next_g = 0.0f;
+    double total = 0.0;
+    auto fetch_rows = [&](int c) {
+        const int at = chunk_at(c), rows = chunk_rows(at), i = lane < rows ? lane : rows - 1;
+        const int r = lo + at + (dir > 0 ? i : rows - 1 - i);
+        next_seq = A.spans.info[r];
+        int rg = A.shift ? r - dir : r;  // (where that is another sequence's it is not used)
+        rg = rg < olo ? olo : rg >= ohi ? ohi - 1 : rg;
+        next_g = A.gs ? A.g[(long long)rg * A.gs + h] : A.g[h];
+    };
+    auto put_rows = [&](ChunkRows &W, int c) {
+        const int at = chunk_at(c), rows = chunk_rows(at), i = lane;
+        const int r = lo + at + (dir > 0 ? i : rows - 1 - i);
+        int f = dir > 0 ? next_seq.x - (r - i) : (r + i) - (next_seq.y - 1), l = dir > 0 ? next_seq.y - 1 - (r - i) : (r + i) - next_seq.x;
+        if (i >= rows) f = l = i;  // behind the last row: on its own
+        const float g = next_g < kForget ? kForget : next_g;  // (NaN stays)
+        double b = i >= rows || (A.shift && f == i) ? 0.0 : (double)g * 1.4426950408889634;
+        const int from = f > 0 ? f : 0;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const double o = __shfl_up(b, d);
+            if (i - d >= from) b += o;
+        }
+        const int e = l < rows - 1 ? l : rows - 1;
+        const double be = __shfl(b, e & 63);
+        const float bf = (float)b, de = exp2_of(b);
+        W.bh[i] = bf, W.bl[i] = (float)(b - (double)bf);
+        W.decay[i] = de, W.in[i] = A.out_scale * de, W.to[i] = A.kv_scale * exp2_of(be - b);
+        W.seg[i] = (f < 0 ? 0 : f + 1) | (i < rows ? e + 1 : i + 1) << 8 | (l <= rows - 1 ? 1 << 16 : 0);
+        if (!OUT) total += __shfl(b, rows - 1);
     };
     fetch(0);
-    double total = 0.0;
+    if (wave == NW - 1) {
+        fetch_rows(0);
+        put_rows(rows_of[0], 0);
+        if (chunks > 1) fetch_rows(1);
+    }
+    if (OUT)  // the weights above the diagonal that share a fragment with some below
+        for (int i = tid; i < kChunk * LP * (int)sizeof(ME) / 4; i += NT) ((unsigned *)Ps)[i] = 0;
 
     for (int c = 0; c < chunks; ++c) {
-        int row0, rows;
-        chunk_at(c, row0, rows);
-        if (OUT) tq.store(Qs, tid);
-        tk.store(Ks, tid);
-        tv.store(Vs, tid);
-        if (DOT) tx.store(Xs, tid);
-        const int wild = tk.infinite() || tv.infinite();
-        if (wave == 0) {
-            // The chunk's rows: where their sequences begin and end in it, and the sums of their log decays from there.
-            const int i = lane, r = row0 + dir * i;
-            const int2 s = i < rows ? A.spans.info[r] : int2{-1, -1};
-            const bool live = s.x >= 0;
-            int f = i, l = i;
-            if (live) f = dir > 0 ? s.x - row0 : row0 - (s.y - 1), l = dir > 0 ? s.y - 1 - row0 : row0 - s.x;
-            double b = 0.0;
-            if (live && !(A.shift && f == i)) b = (double)log_decay_of(A, A.shift ? r - dir : r, h);
-            const int from = f > 0 ? f : 0;
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const double o = __shfl_up(b, d);
-                if (i - d >= from) b += o;
-            }
-            const int e = l < rows - 1 ? l : rows - 1;
-            const double be = __shfl(b, e & 63), w = be - b;
-            const float bf = (float)b, bg = (float)(b - (double)bf), wf = (float)w, wg = (float)(w - (double)wf);
-            bh[i] = bf, bl[i] = bg;
-            const float eb = expf(bf), ew = expf(wf);
-            fo[i] = A.out_scale * (eb + eb * bg);
-            wt[i] = A.kv_scale * (ew + ew * wg);
-            endd[i] = eb + eb * bg;
-            first[i] = live ? f : 64;
-            past[i] = live ? e + 1 : i + 1;
-            stat[i] = (live ? 1 : 0) | (live && l <= rows - 1 ? 2 : 0);
-            total += __shfl(b, rows - 1);
-        }
-        const bool slow = __syncthreads_or(wild);
+        const int at = chunk_at(c), rows = chunk_rows(at);
+        const ChunkRows &W = rows_of[c & 1];
+        if (OUT) tq.store(Qs, rows, dir, tid);
+        tk.store(Ks, rows, dir, tid);
+        tv.store(Vs, rows, dir, tid);
+        if (DOT) tx.store(Xs, rows, dir, tid);
+        const bool slow = __syncthreads_or(tk.infinite() || tv.infinite());
         if (c + 1 < chunks) fetch(c + 1);
 
         if (OUT) {
             // weights: tile (s tile ms, t tile mt), transposed, so that four consecutive s of a row t land in a lane
-            constexpr int tiles = 10;
-            for (int w = wave; w < tiles; w += NW) {
+            const float sc = A.out_scale * A.kv_scale;
+#pragma unroll 1
+            for (int w = wave; w < 10; w += NW) {
                 const int mt = w < 4 ? 3 : w < 7 ? 2 : w < 9 ? 1 : 0, ms = w < 4 ? w : w < 7 ? w - 4 : w < 9 ? w - 7 : 0;
-                o_f32x4 a = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int k0 = 0; k0 < DK; k0 += KM)
-                    a = M::mma(M::along(Ks, LK, 16 * ms + n, k0, q), M::along(Qs, LK, 16 * mt + n, k0, q), a);
-                const int t = 16 * mt + n, s = 16 * ms + 4 * q, f = first[t];
-                const float th = bh[t], tl = bl[t];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float e = A.out_scale * A.kv_scale * expf((th - bh[s + i]) + (tl - bl[s + i]));
-                    a[i] = s + i <= t && s + i >= f ? a[i] * e : 0.0f;
-                }
+                const int t = 16 * mt + n, s = 16 * ms + 4 * q, f = seg_first(W.seg[t]);
+                const bool apart = seg_first(__builtin_amdgcn_readfirstlane(W.seg[16 * mt])) >= 16 * ms + 16;  // all of the tile's rows are of later sequences
                 typedef __attribute__((ext_vector_type(4))) ME V4;
-                *(V4 *)(Ps + t * LP + s) = __builtin_convertvector(a, V4);
-                if (PAIRS) {
-                    // products of dq's weights with q k: their sums by t and by s are what q dq and k dk have of them
-                    o_f32x4 z = {0.f, 0.f, 0.f, 0.f};
+                o_f32x4 a = {0.f, 0.f, 0.f, 0.f};
+                if (!apart) {
 #pragma unroll
-                    for (int k0 = 0; k0 < DV; k0 += KM)
-                        z = M::mma(M::along(Vs, LV, 16 * ms + n, k0, q), M::along(Xs, LV, 16 * mt + n, k0, q), z);
-                    float col[4], row = 0.0f;
+                    for (int k0 = 0; k0 < DK; k0 += KM)
+                        a = M::mma(M::along(Ks, LK, 16 * ms + n, k0, q), M::along(Qs, LK, 16 * mt + n, k0, q), a);
+                    const float th = W.bh[t], tl = W.bl[t];
+                    const o_f32x4 sh = *(const o_f32x4 *)&W.bh[s], sl = *(const o_f32x4 *)&W.bl[s];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        col[i] = s + i <= t && s + i >= f ? a[i] * z[i] : 0.0f;
-                        row += col[i];
+                        const float e = exp2_hw((th - sh[i]) + (tl - sl[i]));
+                        a[i] = s + i <= t && s + i >= f ? a[i] * (e * sc) : 0.0f;
+                    }
+                }
+                *(V4 *)(Ps + t * LP + s) = __builtin_convertvector(a, V4);
+                if (pairs) {
+                    // products of dq's weights with q k: their sums by t and by s are what q dq and k dk have of them
+                    o_f32x4 z = {0.f, 0.f, 0.f, 0.f};
+                    if (!apart) {
+#pragma unroll
+                        for (int k0 = 0; k0 < DV; k0 += KM)
+                            z = M::mma(M::along(Vs, LV, 16 * ms + n, k0, q), M::along(Xs, LV, 16 * mt + n, k0, q), z);
+                    }
+                    float row = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        z[i] = s + i <= t && s + i >= f ? a[i] * z[i] : 0.0f;
+                        row += z[i];
                     }
                     row += __shfl_xor(row, 16);
                     row += __shfl_xor(row, 32);
                     if (q == 0) rowp[ms][t] = row;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int d = 1; d < 16; d *= 2)
 #pragma unroll
-                        for (int d = 1; d < 16; d *= 2) col[i] += __shfl_xor(col[i], d);
-                        if (n == 0) colp[mt][s + i] = col[i];
-                    }
+                        for (int i = 0; i < 4; ++i) z[i] += __shfl_xor(z[i], d);
+                    if (n == 0) *(o_f32x4 *)&colp[mt][s] = z;
                 }
             }
             __syncthreads();
@@ -419,58 +481,62 @@ __global__ __launch_bounds__(4 * DV) void tf_decay_span_kernel(DecayRun A) {
         o_f32x4 o[4];
 #pragma unroll
         for (int m = 0; m < 4; ++m) o[m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
-        // The chunk's sequences, one after the other: what their state adds to their rows, and the state after them.
+        // The chunk's sequences, one after the other: what their state adds to their rows, and the state after them.  Those
+        // that are whole in the chunk have none, unless states come in or go out.
+#pragma unroll 1
         for (int a = 0; a < rows;) {
-            const int b = __builtin_amdgcn_readfirstlane(past[a]), st = __builtin_amdgcn_readfirstlane(stat[a]);
-            if (!(st & 1)) {
-                a = b;
-                continue;
-            }
-            const bool starts = __builtin_amdgcn_readfirstlane(first[a]) == a, ends = st & 2;
+            const int seg = __builtin_amdgcn_readfirstlane(W.seg[a]), b = seg_past(seg);
+            const bool starts = seg_first(seg) >= 0, ends = seg_ends(seg);
             int seq = -1;
-            if ((starts && A.s0) || (ends && A.sf)) seq = seq_of_row(A.offsets, A.n_seqs, row0 + dir * a);
+            if ((starts && A.s0) || (ends && A.sf))
+                seq = seq_of_row(A.offsets, A.n_seqs, lo + at + (dir > 0 ? a : rows - 1 - a));
             if (starts) {
                 have = A.s0 != nullptr;
                 if (have) load_state(A.s0 + ((long long)seq * A.heads + h) * (DK * DV));
             }
             if (OUT && have) {
-                F sp[DK / KM][NS];
+                o_f32x4 z[4];
+#pragma unroll
+                for (int m = 0; m < 4; ++m) z[m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int k = 0; k < DK / KM; ++k) {
                     float x[4 * M::TILES];
 #pragma unroll
                     for (int i = 0; i < 4 * M::TILES; ++i) x[i] = S[k * M::TILES + i / 4][i % 4];
-                    M::template split<NS>(x, sp[k]);
+                    F sp[NS];
+                    M::template split<NS>(x, sp);
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        if (16 * m + 16 <= a || 16 * m >= b) continue;
+                        const F f = M::along_state(Qs, LK, 16 * m + n, k * KM, q);
+#pragma unroll
+                        for (int j = NS - 1; j >= 0; --j) z[m] = M::mma(sp[j], f, z[m]);
+                    }
                 }
 #pragma unroll
                 for (int m = 0; m < 4; ++m) {
-                    if (16 * m + 16 <= a || 16 * m >= b) continue;
-                    o_f32x4 z = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int k = 0; k < DK / KM; ++k) {
-                        const F f = M::along_state(Qs, LK, 16 * m + n, k * KM, q);
-#pragma unroll
-                        for (int j = NS - 1; j >= 0; --j) z = M::mma(sp[k][j], f, z);
-                    }
                     const int t = 16 * m + n;
-                    const float f = fo[t];
+                    const float f = W.in[t];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[m][i] = t >= a && t < b ? z[i] * f : o[m][i];
+                    for (int i = 0; i < 4; ++i) o[m][i] = t >= a && t < b ? z[m][i] * f : o[m][i];
                 }
             }
             if (!ends || A.sf) {
-                const float d = endd[b - 1];
+                const float d = W.decay[b - 1];
 #pragma unroll
                 for (int m = 0; m < ST; ++m) S[m] = have ? S[m] * d : o_f32x4{0.f, 0.f, 0.f, 0.f};
                 if (!slow) {
 #pragma unroll
                     for (int k = 0; k < NB; ++k) {
+                        if (k * KM + KM <= a || k * KM >= b) continue;
                         const F v = M::down(Vs, LV, k * KM, c0, n, q);
                         float x[KM / 4];
 #pragma unroll
-                        for (int i = 0; i < KM / 4; ++i) {
+                        for (int i = 0; i < KM / 4; i += 4) {
                             const int s = k * KM + KM / 4 * q + i;
-                            x[i] = s >= a && s < b ? (float)v[i] * wt[s] : 0.0f;
+                            const o_f32x4 w = *(const o_f32x4 *)&W.to[s];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) x[i + j] = s + j >= a && s + j < b ? (float)v[i + j] * w[j] : 0.0f;
                         }
                         F vp[NU];
                         M::template split<NU>(x, vp);
@@ -482,8 +548,9 @@ __global__ __launch_bounds__(4 * DV) void tf_decay_span_kernel(DecayRun A) {
                         }
                     }
                 } else {
+#pragma unroll 1
                     for (int s = a; s < b; ++s) {
-                        const float v = (float)Vs[s * LV + c0 + n] * wt[s];
+                        const float v = (float)Vs[s * LV + c0 + n] * W.to[s];
 #pragma unroll
                         for (int m = 0; m < ST; ++m)
 #pragma unroll
@@ -494,25 +561,30 @@ __global__ __launch_bounds__(4 * DV) void tf_decay_span_kernel(DecayRun A) {
                 if (ends && A.sf) {
                     float *s = A.sf + ((long long)seq * A.heads + h) * (DK * DV);
                     float d = 1.0f;
-                    if (A.sf_decay) d = expf(log_decay_of(A, row0 + dir * (b - 1), h));
+                    if (A.sf_decay) d = expf(log_decay_of(A, lo + at + (dir > 0 ? b - 1 : rows - b), h));
+                    const int step = A.turned ? 1 : DV;
+                    float *e = s + (A.turned ? (c0 + n) * DK + 4 * q : 4 * q * DV + c0 + n);
 #pragma unroll
                     for (int m = 0; m < ST; ++m)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int e = 16 * m + 4 * q + i, f = c0 + n;
-                            s[A.turned ? f * DK + e : e * DV + f] = S[m][i] * d;
-                        }
+                        for (int i = 0; i < 4; ++i) e[(16 * m + i) * step] = S[m][i] * d;
                 }
             }
             a = b;
+            if (!A.s0 && !A.sf && b < rows) {  // on to the last one
+                const int f = seg_first(__builtin_amdgcn_readfirstlane(W.seg[rows - 1]));
+                if (f > b) a = f;
+            }
         }
         if (OUT) {
             if (DOT) {
 #pragma unroll
                 for (int m = 0; m < 4; ++m) {
                     float z = 0.0f;
+                    typedef __attribute__((ext_vector_type(4))) ME V4;
+                    const o_f32x4 x = __builtin_convertvector(*(const V4 *)(Xs + (16 * m + n) * LV + c0 + 4 * q), o_f32x4);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) z += o[m][i] * (float)Xs[(16 * m + n) * LV + c0 + 4 * q + i];
+                    for (int i = 0; i < 4; ++i) z += o[m][i] * x[i];
                     z += __shfl_xor(z, 16);
                     z += __shfl_xor(z, 32);
                     if (q == 0) dots[wave][16 * m + n] = z;
@@ -530,83 +602,152 @@ __global__ __launch_bounds__(4 * DV) void tf_decay_span_kernel(DecayRun A) {
                 // an infinite or NaN k or v: only the products that the definition has
 #pragma unroll
                 for (int m = 0; m < 4; ++m) {
-                    const int t = 16 * m + n, f = first[t] > 0 ? first[t] : 0;
-                    for (int s = f; s <= t; ++s)
+                    const int t = 16 * m + n, f = seg_first(W.seg[t]);
+                    for (int s = f > 0 ? f : 0; s <= t; ++s)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) o[m][i] += (float)Ps[t * LP + s] * (float)Vs[s * LV + c0 + 4 * q + i];
                 }
             }
+            // (the chunk's first row is a scalar; 64 rows of a stride fit in 32 bits)
+            const int es = A.out_f32 ? 4 : ES;
+            char *ob = (char *)A.out + ((long long)(lo + at) * A.os + h * DV + c0) * es;
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
                 const int t = 16 * m + n;
-                if (t < rows && (stat[t] & 1)) {
-                    const long long at = (long long)(row0 + dir * t) * A.os + h * DV + c0 + 4 * q;
-                    if (A.out_f32) *(o_f32x4 *)((float *)A.out + at) = o[m];
-                    else store4<T>((typename T::E *)A.out + at, o[m]);
+                if (t < rows) {
+                    char *to = ob + (unsigned)((dir > 0 ? t : rows - 1 - t) * (int)A.os + 4 * q) * (unsigned)es;
+                    if (A.out_f32) *(o_f32x4 *)to = o[m];
+                    else store4<T>((typename T::E *)to, o[m]);
                 }
             }
+        }
+        if (wave == NW - 1 && c + 1 < chunks) {
+            put_rows(rows_of[(c + 1) & 1], c + 1);
+            if (c + 2 < chunks) fetch_rows(c + 2);
         }
         __syncthreads();
         if (DOT && wave == 0) {
             const int t = lane;
-            if (t < rows && (stat[t] & 1)) {
+            if (t < rows) {
                 float z = 0.0f;
                 for (int w = 0; w < NW; ++w) z += dots[w][t];
-                if (PAIRS)
+                if (pairs)
                     for (int m = 0; m < 4; ++m) {
                         if (m <= t / 16) z += rowp[m][t];
                         if (m >= t / 16) z -= colp[m][t];
                     }
-                A.db[(long long)(row0 + dir * t) * A.heads + h] = z;
+                A.db[(long long)(lo + at + (dir > 0 ? t : rows - 1 - t)) * A.heads + h] = z;
             }
         }
     }
     if (!OUT) {
-        float *s = A.local + ((long long)p * A.heads + h) * (DK * DV);
+        float *s = A.local + ((long long)p * A.heads + h) * (DK * DV) + 4 * q * DV + c0 + n;
 #pragma unroll
         for (int m = 0; m < ST; ++m)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[(16 * m + 4 * q + i) * DV + c0 + n] = S[m][i];
-        if (tid == 0) A.mult[(long long)p * A.heads + h] = whole ? expf((float)total) : 0.0f;
+            for (int i = 0; i < 4; ++i) s[(16 * m + i) * DV] = S[m][i];
+        if (wave == NW - 1 && lane == 0) A.mult[(long long)p * A.heads + h] = whole ? exp2_of(total) : 0.0f;
     }
 }
 
-// First and past-the-last row of every row's sequence; whether the offsets are in order and inside the array.
+// First and past-the-last row of every row's sequence; whether the offsets are in order and inside the array.  A workgroup
+// has 1024 rows: it finds the sequence of the first by 256 probes at a time, puts the starts of the sequences that follow
+// where they are, and a running maximum tells every row its sequence (a thread a row and a binary search each took 92 us
+// for 918 161 rows of 65 536 sequences).
 __global__ __launch_bounds__(256) void tf_decay_index_kernel(const int32_t *__restrict__ offsets, int n_seqs, int n_rows,
                                                              int2 *__restrict__ info, int *__restrict__ bad,
                                                              int32_t *__restrict__ flags) {
-    if (blockIdx.x == 0) {
+    __shared__ int mark[kIndexRows], top[4];
+    const int tid = threadIdx.x;
+    if (blockIdx.x < kCheckers) {
         int wrong = 0;
-        for (int i = threadIdx.x; i <= n_seqs; i += 256) {
-            const int o = offsets[i];
-            wrong |= o < 0 || o > n_rows || (i < n_seqs && offsets[i + 1] < o);
+#pragma unroll 8
+        for (int i = blockIdx.x * 256 + tid; i <= n_seqs; i += 256 * kCheckers) {
+            const int o = offsets[i], e = offsets[i < n_seqs ? i + 1 : i];
+            wrong |= o < 0 || o > n_rows || e < o;
         }
         wrong = __syncthreads_or(wrong);
-        if (threadIdx.x == 0) {
-            *bad = wrong;
+        if (tid == 0) {
+            bad[blockIdx.x] = wrong;
             if (wrong && flags) atomicOr(flags, TF_SEQ_BAD_OFFSETS);
         }
         return;
     }
-    const long long r = (long long)(blockIdx.x - 1) * 256 + threadIdx.x;
-    if (r >= n_rows) return;
-    const int s = seq_of_row(offsets, n_seqs, r);
-    info[r] = s < 0 ? int2{-1, -1} : int2{offsets[s], offsets[s + 1]};
+    const int r0 = (int)(blockIdx.x - kCheckers) * kIndexRows, r1 = n_rows - r0 < kIndexRows ? n_rows : r0 + kIndexRows;
+    // how many of the n_seqs + 1 offsets are at most r0
+    int lo = 0, hi = n_seqs + 1;
+    while (lo < hi) {
+        const int step = (hi - lo + 255) / 256, i = lo + tid * step;
+        const int below = __syncthreads_count(i < hi && offsets[i] <= r0);  // these are the first ones
+        if (below == 0) break;
+        const int end = lo + below * step;
+        lo = lo + (below - 1) * step + 1;
+        hi = end < hi ? end : hi;
+    }
+#pragma unroll
+    for (int j = 0; j < kIndexRows / 256; ++j) mark[tid + 256 * j] = 0;
+    __syncthreads();
+    for (int i = lo;; i += 256) {  // the offsets behind r0, to the tile's end
+        const int o = i + tid <= n_seqs ? offsets[i + tid] : n_rows;
+        if (o > r0 && o < r1) atomicMax(&mark[o - r0], i + tid + 1);  // offsets at most this row's
+        if (__syncthreads_count(i + tid <= n_seqs && o < r1) < 256) break;
+    }
+    int m[4], best = tid == 0 ? lo : 0;
+    const int4 four = *(const int4 *)&mark[4 * tid];
+    m[0] = four.x, m[1] = four.y, m[2] = four.z, m[3] = four.w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m[j] = best = best > m[j] ? best : m[j];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int o = __shfl_up(best, d);
+        if (tid % 64 >= d && o > best) best = o;
+    }
+    if (tid % 64 == 63) top[tid / 64] = best;
+    __syncthreads();
+    int before = __shfl_up(best, 1);
+    if (tid % 64 == 0) before = 0;
+    for (int w = 0; w < tid / 64; ++w) before = before > top[w] ? before : top[w];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = r0 + 4 * tid + j, k = m[j] > before ? m[j] : before;
+        if (r < n_rows) info[r] = k == 0 || k > n_seqs ? int2{-1, -1} : int2{offsets[k - 1], offsets[k]};
+    }
 }
 
-// The states at the spans' ends from the spans' own contributions, in order along each cut sequence.
-__global__ __launch_bounds__(256) void tf_decay_chain_kernel(float *__restrict__ local, const float *__restrict__ mult,
-                                                             const int *__restrict__ kind, int n_spans, int heads, int size,
-                                                             int dir, const int *bad) {
-    if (*bad) return;
+// The states at the spans' ends from the spans' own contributions, in order along each cut sequence: a workgroup has
+// 1024 values of the states of one sequence's cuts and head, from its first.  The next spans' contributions are read while
+// the sum is on its way.
+__global__ __launch_bounds__(256) void tf_decay_chain_kernel(DecayRuns R, int size) {
+    const DecayRun &A = R.run[blockIdx.z];
+    if (any_bad(A.bad)) return;
+    const int heads = A.heads, spans = A.spans.n, dir = A.dir;
     const int p = blockIdx.x / heads, h = blockIdx.x % heads, e = (blockIdx.y * 256 + threadIdx.x) * 4;
-    if (kind[p] != 1 || e >= size) return;  // a sequence's first cut
-    o_f32x4 s = *(const o_f32x4 *)(local + ((long long)p * heads + h) * size + e);
-    for (int i = p + dir; i >= 0 && i < n_spans && kind[i] == 2; i += dir) {
-        const long long at = (long long)i * heads + h;
-        o_f32x4 *l = (o_f32x4 *)(local + at * size + e);
-        s = *l + s * mult[at];
-        *l = s;
+    if (A.kind[p] != 1) return;  // a sequence's first cut
+    int cuts = 0;
+    for (int i = p + dir; i >= 0 && i < spans; i += 64 * dir) {  // how many spans it goes on through whole
+        const int j = i + dir * (int)(threadIdx.x % 64);
+        const unsigned long long on = __ballot(j >= 0 && j < spans && A.kind[j < 0 ? 0 : j < spans ? j : spans - 1] == 2);
+        const int run = ~on ? __builtin_ctzll(~on) : 64;
+        cuts += run;
+        if (run < 64) break;
+    }
+    const long long step = (long long)dir * heads * size;
+    float *l = A.local + ((long long)p * heads + h) * size + e;
+    const float *m = A.mult + (long long)p * heads + h;
+    o_f32x4 s = *(const o_f32x4 *)l;
+    constexpr int AHEAD = 8;
+    for (int i = 0; i < cuts; i += AHEAD) {
+        o_f32x4 x[AHEAD];
+        float w[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (i + j < cuts) x[j] = *(const o_f32x4 *)(l + (i + j + 1) * step), w[j] = m[(long long)(i + j + 1) * dir * heads];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (i + j < cuts) {
+                s = x[j] + s * w[j];
+                *(o_f32x4 *)(l + (i + j + 1) * step) = s;
+            }
     }
 }
 
@@ -614,7 +755,7 @@ __global__ __launch_bounds__(256) void tf_decay_chain_kernel(float *__restrict__
 __global__ __launch_bounds__(256) void tf_decay_empty_kernel(const int32_t *__restrict__ offsets, int n_seqs, long long size,
                                                              const float *__restrict__ s0, float *__restrict__ sf,
                                                              const int *bad) {
-    const bool wrong = *bad;
+    const bool wrong = any_bad(bad);
     for (int i = blockIdx.x; i < n_seqs; i += gridDim.x) {
         if (!wrong && offsets[i] != offsets[i + 1]) continue;
         for (long long e = threadIdx.x; e < size; e += 256)
@@ -644,7 +785,7 @@ struct DecayGrad {
 
 // Inner products of states and their gradients: a wave each, of the cut borders and of the sequences' ends.
 __global__ __launch_bounds__(256) void tf_decay_dots_kernel(DecayGrad A) {
-    if (*A.bad) return;
+    if (any_bad(A.bad)) return;
     const long long item = (long long)blockIdx.x * 4 + threadIdx.x / 64, borders = (long long)A.spans.n * A.heads;
     const int lane = threadIdx.x % 64;
     const float *a, *b;
@@ -681,7 +822,7 @@ __global__ __launch_bounds__(256) void tf_decay_dots_kernel(DecayGrad A) {
 // its first, sequence by sequence.  The sums are fp64, so that rows far from the end lose nothing.
 __global__ __launch_bounds__(64) void tf_decay_grad_kernel(DecayGrad A) {
     const int p = blockIdx.x / A.heads, h = blockIdx.x % A.heads, i = threadIdx.x, dir = -A.dir;
-    if (*A.bad) {
+    if (any_bad(A.bad)) {
         const float nan = __builtin_nanf("");
         const long long lo = (long long)p * A.spans.span;
         const long long hi = lo + A.spans.span < A.spans.n_rows ? lo + A.spans.span : A.spans.n_rows;
@@ -741,7 +882,8 @@ __global__ __launch_bounds__(256) void tf_decay_share_kernel(const float *__rest
                                                              long long n_rows, const int32_t *__restrict__ offsets, int n_seqs,
                                                              typename T::E *__restrict__ out, long long stride, const int *bad) {
     const int per = shared * width / 4;
-    const long long lo = *bad ? 0 : offsets[0], hi = *bad ? n_rows : offsets[n_seqs];
+    const bool wrong = any_bad(bad);
+    const long long lo = wrong ? 0 : offsets[0], hi = wrong ? n_rows : offsets[n_seqs];
     for (long long i = lo * per + (long long)blockIdx.x * 256 + threadIdx.x; i < hi * per; i += (long long)gridDim.x * 256) {
         const long long r = i / per;
         const int c = (int)(i - r * per) * 4, hk = c / width, d = c - hk * width;
@@ -838,7 +980,7 @@ Plan decay_plan(const tf_decay_config *c, int64_t n_rows, int64_t n_seqs, bool b
     Room r(base);
     Plan p = {};
     const int64_t spans = decay_spans(c, n_rows), h = c->n_heads, size = (int64_t)c->d_k * c->d_v;
-    p.bad = r.take<int>(1);
+    p.bad = r.take<int>(kCheckers);
     p.info = r.take<int2>(n_rows);
     for (int i = 0; i < (back ? 2 : 1); ++i) {
         p.kind[i] = r.take<int>(spans);
@@ -863,41 +1005,40 @@ Plan decay_plan(const tf_decay_config *c, int64_t n_rows, int64_t n_seqs, bool b
     return p;
 }
 
-template <class T, int DK, int DV> void span_mode(const DecayRun &A, int mode, hipStream_t s) {
-    const dim3 grid((unsigned)(A.spans.n * A.heads)), block(4 * DV);
+template <class T, int DK, int DV> void span_mode(const DecayRuns &R, int runs, int mode, hipStream_t s) {
+    const dim3 grid((unsigned)(R.run[0].spans.n * R.run[0].heads), runs), block(4 * DV);
     switch (mode) {
-        case DECAY_STATE: hipLaunchKernelGGL((tf_decay_span_kernel<T, DK, DV, DECAY_STATE>), grid, block, 0, s, A); break;
-        case DECAY_OUT: hipLaunchKernelGGL((tf_decay_span_kernel<T, DK, DV, DECAY_OUT>), grid, block, 0, s, A); break;
-        case DECAY_DOT: hipLaunchKernelGGL((tf_decay_span_kernel<T, DK, DV, DECAY_DOT>), grid, block, 0, s, A); break;
-        default: hipLaunchKernelGGL((tf_decay_span_kernel<T, DK, DV, DECAY_PAIRS>), grid, block, 0, s, A); break;
+        case DECAY_STATE: hipLaunchKernelGGL((tf_decay_span_kernel<T, DK, DV, DECAY_STATE>), grid, block, 0, s, R); break;
+        case DECAY_OUT: hipLaunchKernelGGL((tf_decay_span_kernel<T, DK, DV, DECAY_OUT>), grid, block, 0, s, R); break;
+        default: hipLaunchKernelGGL((tf_decay_span_kernel<T, DK, DV, DECAY_DOT>), grid, block, 0, s, R); break;
     }
 }
-template <class T, int DK> void span_dv(const DecayRun &A, int dv, int mode, hipStream_t s) {
-    if (dv == 32) span_mode<T, DK, 32>(A, mode, s);
-    else if (dv == 64) span_mode<T, DK, 64>(A, mode, s);
-    else span_mode<T, DK, 128>(A, mode, s);
+template <class T, int DK> void span_dv(const DecayRuns &R, int runs, int dv, int mode, hipStream_t s) {
+    if (dv == 32) span_mode<T, DK, 32>(R, runs, mode, s);
+    else if (dv == 64) span_mode<T, DK, 64>(R, runs, mode, s);
+    else span_mode<T, DK, 128>(R, runs, mode, s);
 }
-template <class T> void span_dk(const DecayRun &A, int dk, int dv, int mode, hipStream_t s) {
-    if (dk == 32) span_dv<T, 32>(A, dv, mode, s);
-    else if (dk == 64) span_dv<T, 64>(A, dv, mode, s);
-    else span_dv<T, 128>(A, dv, mode, s);
+template <class T> void span_dk(const DecayRuns &R, int runs, int dk, int dv, int mode, hipStream_t s) {
+    if (dk == 32) span_dv<T, 32>(R, runs, dv, mode, s);
+    else if (dk == 64) span_dv<T, 64>(R, runs, dv, mode, s);
+    else span_dv<T, 128>(R, runs, dv, mode, s);
 }
-void span_run(int elem, const DecayRun &A, int dk, int dv, int mode, hipStream_t s) {
-    if (elem == TF_ELEM_BF16) span_dk<ElemBF16>(A, dk, dv, mode, s);
-    else if (elem == TF_ELEM_FP32) span_dk<ElemF32>(A, dk, dv, mode, s);
-    else span_dk<ElemF16>(A, dk, dv, mode, s);
+void span_run(int elem, const DecayRuns &R, int runs, int dk, int dv, int mode, hipStream_t s) {
+    if (elem == TF_ELEM_BF16) span_dk<ElemBF16>(R, runs, dk, dv, mode, s);
+    else if (elem == TF_ELEM_FP32) span_dk<ElemF32>(R, runs, dk, dv, mode, s);
+    else span_dk<ElemF16>(R, runs, dk, dv, mode, s);
 }
-// The states at the spans' ends of a run whose arguments k, v, g, s0 are set.
-void chain_run(int elem, DecayRun A, int dk, int dv, hipStream_t s) {
+// The states at the spans' ends of runs whose arguments k, v, g, s0 are set.
+void chain_run(int elem, DecayRuns R, int runs, int dk, int dv, hipStream_t s) {
+    const DecayRun &A = R.run[0];
     if (A.spans.n < 2) return;
-    A.sf = nullptr;
-    A.turned = 0;
-    span_run(elem, A, dk, dv, DECAY_STATE, s);
-    hipLaunchKernelGGL(tf_decay_chain_kernel, dim3((unsigned)(A.spans.n * A.heads), (unsigned)(dk * dv / 1024)), dim3(256), 0, s,
-                       A.local, A.mult, A.kind, A.spans.n, A.heads, dk * dv, A.dir, A.bad);
+    for (int i = 0; i < runs; ++i) R.run[i].sf = nullptr, R.run[i].turned = 0;
+    span_run(elem, R, runs, dk, dv, DECAY_STATE, s);
+    hipLaunchKernelGGL(tf_decay_chain_kernel, dim3((unsigned)(A.spans.n * A.heads), (unsigned)(dk * dv / 1024), runs), dim3(256), 0, s, R,
+                       dk * dv);
 }
 void index_run(const int32_t *offsets, int n_seqs, int64_t n_rows, const Plan &p, int32_t *flags, hipStream_t s) {
-    hipLaunchKernelGGL(tf_decay_index_kernel, dim3((unsigned)(1 + (n_rows + 255) / 256)), dim3(256), 0, s, offsets, n_seqs,
+    hipLaunchKernelGGL(tf_decay_index_kernel, dim3((unsigned)(kCheckers + (n_rows + kIndexRows - 1) / kIndexRows)), dim3(256), 0, s, offsets, n_seqs,
                        (int)n_rows, p.info, p.bad, flags);
 }
 void empty_run(const int32_t *offsets, int n_seqs, long long size, const float *s0, float *sf, const Plan &p, hipStream_t s) {
@@ -921,7 +1062,14 @@ void share_run(const float *part, const tf_decay_config *c, int64_t n_rows, cons
 
 bool decay_sizes_ok(const tf_decay_config *c, int64_t n_rows, int32_t n_seqs) {
     // rows are 32-bit numbers, and so are workgroups
-    return n_rows <= INT32_MAX - 2 * kChunk && decay_spans(c, n_rows) * c->n_heads < INT32_MAX;
+    return n_rows <= INT32_MAX - 2048 && decay_spans(c, n_rows) * c->n_heads < INT32_MAX;
+}
+
+// A chunk's rows are addressed by 32-bit offsets.
+bool strides_fit(std::initializer_list<int64_t> strides) {
+    for (int64_t s : strides)
+        if (s > (1 << 24)) return false;
+    return true;
 }
 
 }  // namespace
@@ -948,7 +1096,7 @@ extern "C" tf_status tf_decay_attention(const tf_decay_config *c, const void *q,
     if (!stride_ok(q_stride, qw, c->elem) || !stride_ok(k_stride, qw, c->elem) || !stride_ok(v_stride, vw, c->elem) ||
         !stride_ok(out_stride, vw, c->elem))
         return TF_EINVAL;
-    if (!decay_sizes_ok(c, n_rows, n_seqs)) return TF_EUNSUPPORTED;
+    if (!decay_sizes_ok(c, n_rows, n_seqs) || !strides_fit({q_stride, k_stride, v_stride, out_stride})) return TF_EUNSUPPORTED;
     if (n_seqs == 0) return TF_OK;
     if (!offsets || !workspace) return TF_EINVAL;
     if (n_rows > 0 && (!q || !k || !v || !out || !log_decay)) return TF_EINVAL;
@@ -970,8 +1118,9 @@ extern "C" tf_status tf_decay_attention(const tf_decay_config *c, const void *q,
         A.out_scale = c->scale, A.kv_scale = 1.0f;
         A.offsets = offsets, A.n_seqs = n_seqs, A.heads = c->n_heads, A.dir = c->reverse ? -1 : 1, A.bad = p.bad;
         A.spans = {p.info, (int)n_rows, decay_span(c, n_rows), (int)decay_spans(c, n_rows)};
-        chain_run(c->elem, A, c->d_k, c->d_v, stream);
-        span_run(c->elem, A, c->d_k, c->d_v, DECAY_OUT, stream);
+        const DecayRuns R = {{A, A}};
+        chain_run(c->elem, R, 1, c->d_k, c->d_v, stream);
+        span_run(c->elem, R, 1, c->d_k, c->d_v, DECAY_OUT, stream);
     }
     return hipGetLastError() == hipSuccess ? TF_OK : TF_EHIP;
 }
@@ -991,7 +1140,9 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
         !stride_ok(d_out_stride, vw, c->elem) || !stride_ok(dq_stride, qw, c->elem) || !stride_ok(dk_stride, qw, c->elem) ||
         !stride_ok(dv_stride, vw, c->elem))
         return TF_EINVAL;
-    if (!decay_sizes_ok(c, n_rows, n_seqs)) return TF_EUNSUPPORTED;
+    if (!decay_sizes_ok(c, n_rows, n_seqs) ||
+        !strides_fit({q_stride, k_stride, v_stride, d_out_stride, dq_stride, dk_stride, dv_stride}))
+        return TF_EUNSUPPORTED;
     if (!offsets || !workspace || (!decay_stride && !d_log_decay)) return TF_EINVAL;
     if (n_rows > 0 && (!q || !k || !v || !d_out || !dq || !dk || !dv || !log_decay || !d_log_decay)) return TF_EINVAL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(d_out) || !aligned16(dq) || !aligned16(dk) ||
@@ -1013,12 +1164,11 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
         F.k = k, F.ks = k_stride, F.kg = group, F.v = v, F.vs = v_stride, F.vg = 1, F.qg = F.xg = 1;
         F.s0 = initial_state, F.dir = dir, F.out_scale = F.kv_scale = 1.0f;
         F.local = p.local[0], F.mult = p.mult[0], F.kind = p.kind[0];
-        chain_run(c->elem, F, c->d_k, c->d_v, stream);
         DecayRun B = A;
         B.k = q, B.ks = q_stride, B.kg = group, B.v = d_out, B.vs = d_out_stride, B.vg = 1, B.qg = B.xg = 1;
         B.s0 = d_state, B.dir = -dir, B.shift = 1, B.out_scale = 1.0f, B.kv_scale = c->scale;
         B.local = p.local[1], B.mult = p.mult[1], B.kind = p.kind[1];
-        chain_run(c->elem, B, c->d_k, c->d_v, stream);
+        chain_run(c->elem, {{F, B}}, 2, c->d_k, c->d_v, stream);
         const bool shared = group > 1;
         // dq
         DecayRun Q = F;
@@ -1027,8 +1177,7 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
         Q.v = k, Q.vs = k_stride, Q.vg = group;
         Q.x = q, Q.xs = q_stride, Q.xg = group;
         Q.out = shared ? (void *)p.dq : dq, Q.os = shared ? (int64_t)H * c->d_k : dq_stride, Q.out_f32 = shared;
-        Q.turned = 1, Q.sf = p.sl, Q.db = p.da, Q.out_scale = c->scale, Q.kv_scale = 1.0f;
-        span_run(c->elem, Q, c->d_v, c->d_k, DECAY_PAIRS, stream);
+        Q.turned = 1, Q.sf = p.sl, Q.db = p.da, Q.pairs = 1, Q.out_scale = c->scale, Q.kv_scale = 1.0f;
         // dk
         DecayRun K = B;
         K.q = v, K.qs = v_stride, K.qg = 1;
@@ -1037,13 +1186,13 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
         K.x = k, K.xs = k_stride, K.xg = group;
         K.out = shared ? (void *)p.dk : dk, K.os = shared ? (int64_t)H * c->d_k : dk_stride, K.out_f32 = shared;
         K.turned = 1, K.db = p.db;
-        span_run(c->elem, K, c->d_v, c->d_k, DECAY_DOT, stream);
+        span_run(c->elem, {{Q, K}}, 2, c->d_v, c->d_k, DECAY_DOT, stream);
         // dv, and the initial states' gradients
         DecayRun V = B;
         V.q = k, V.qs = k_stride, V.qg = group;
         V.out = dv, V.os = dv_stride;
         V.sf = d_initial, V.sf_decay = 1;
-        span_run(c->elem, V, c->d_k, c->d_v, DECAY_OUT, stream);
+        span_run(c->elem, {{V, V}}, 1, c->d_k, c->d_v, DECAY_OUT, stream);
         if (shared) {
             share_run(p.dq, c, n_rows, offsets, n_seqs, dq, dq_stride, p.bad, stream);
             share_run(p.dk, c, n_rows, offsets, n_seqs, dk, dk_stride, p.bad, stream);
