@@ -46,6 +46,7 @@
 namespace {
 
 constexpr int kChunk = 64;
+constexpr int span_threads(int dv) { return dv == 128 ? 512 : 256; }
 constexpr int kMinSpan = 2 * kChunk;  // borders move by less than a chunk: their order stays
 constexpr float kForget = -200.0f;    // exp of this and less is 0: smaller log decays, -inf too, count as it
 typedef __attribute__((ext_vector_type(4))) short o_s16x4;
@@ -81,17 +82,23 @@ struct MatBF16 {
         return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     }
     static constexpr int TILES = 2;  // state tiles of 16 rows in a fragment
-    // c += a b for fp32 values a (N bf16 parts, the small ones first)
+    // fp32 values as N bf16 parts, each the rest rounded: three hold all 24 bits, two 16 (and sign)
     template <int N> static __device__ __forceinline__ void split(const float *x, F (&p)[N]) {
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+        o_u32x4 w[N];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float r = x[i];
+        for (int i = 0; i < 4; ++i) {
+            f2 r = {x[2 * i], x[2 * i + 1]};
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                p[j][i] = (__bf16)r;
-                r -= (float)p[j][i];
+                const unsigned u = __builtin_bit_cast(unsigned, __builtin_convertvector(r, b2));
+                w[j][i] = u;
+                if (j + 1 < N) r = f2{r[0] - __uint_as_float(u << 16), r[1] - __uint_as_float(u & 0xffff0000u)};
             }
         }
+#pragma unroll
+        for (int j = 0; j < N; ++j) p[j] = __builtin_bit_cast(F, w[j]);
     }
 };
 struct MatF32 {
@@ -133,6 +140,22 @@ __device__ __forceinline__ bool any_bad(const int *__restrict__ bad) {
 #pragma unroll
     for (int i = 0; i < kCheckers; ++i) b |= bad[i];
     return b;
+}
+
+// Steps in order, step(i, fragment i), with the fragments of the next DEPTH - 1 steps on their way.  The fences keep that
+// order: left to itself the compiler reads a fragment, waits for it and only then multiplies, an LDS latency a step.
+template <int N, int DEPTH, class Load, class Step> __device__ __forceinline__ void in_turn(Load load, Step step) {
+    decltype(load(0)) w[DEPTH];
+#pragma unroll
+    for (int i = 0; i < DEPTH - 1; ++i)
+        if (i < N) w[i] = load(i);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (i + DEPTH - 1 < N) w[(i + DEPTH - 1) % DEPTH] = load(i + DEPTH - 1);
+        __builtin_amdgcn_sched_barrier(0);
+        step(i, w[i % DEPTH]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
 // Where the spans' borders are.
@@ -276,31 +299,34 @@ __device__ __forceinline__ int seg_first(int s) { return (s & 255) - 1; }
 __device__ __forceinline__ int seg_past(int s) { return (s >> 8) & 255; }
 __device__ __forceinline__ bool seg_ends(int s) { return s >> 16; }
 
-// One span of one head.  Waves: each owns 16 of the state's and the output's columns; the state
-// stays in its accumulators over the span.  The 64 x 64 weights of a chunk are computed once,
+// One span of one head, four waves.  A wave owns a quarter of the state's and the output's columns (d_v 32: half, and
+// of the outputs every second row tile; its pair holds the same state); the state stays in its accumulators over the span.  The 64 x 64 weights of a chunk are computed once,
 // 16 x 16 tiles on or below the diagonal dealt out to the waves, and pass through LDS.  The next chunk's rows of
 // the tensors are on their way to registers meanwhile, and its row sums are one wave's work beside the products.
 template <class T, int DK, int DV, int MODE>
-__global__ __launch_bounds__(4 * DV, DK * DV <= 64 * 64 && DV == 64 ? 3 : 2) void tf_decay_span_kernel(DecayRuns R) {
+__global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ? 4 : 3) : MODE == DECAY_OUT && DK * DV <= 64 * 64 ? 3 : 2) void tf_decay_span_kernel(DecayRuns R) {
     typedef typename MatOf<T>::M M;
     typedef typename M::E ME;
     typedef typename M::F F;
     constexpr bool OUT = MODE >= DECAY_OUT, DOT = MODE >= DECAY_DOT;
-    constexpr int NW = DV / 16, NT = 64 * NW, KM = M::KM, ES = sizeof(typename T::E);
+    constexpr int NT = span_threads(DV), NW = NT / 64, KM = M::KM, ES = sizeof(typename T::E);
     constexpr int LK = DK + M::PAD, LV = DV + M::PAD, LP = kChunk + M::PAD;
-    constexpr int ST = DK / 16;                    // state tiles of a wave
+    constexpr int CT = 1, RG = DV == 32 ? 2 : 1, TM = 4 / RG;  // column tiles of a wave; waves that share them, and their row tiles
+    constexpr int ST = DK / 16;                    // state tiles of a wave's column tile
     constexpr int NB = kChunk / KM;                // fragments along a chunk's rows
     constexpr int NS = parts_of<M>(DOT ? 3 : 2);   // parts of the state in its product with q
     constexpr int NU = parts_of<M>(3);             // parts of the weighted v in the state's update
     __shared__ __attribute__((aligned(16))) ME Qs[OUT ? kChunk * LK : 8], Ks[kChunk * LK], Vs[kChunk * LV],
         Xs[DOT ? kChunk * LV : 8], Ps[OUT ? kChunk * LP : 8];
     __shared__ ChunkRows rows_of[2];
-    __shared__ float rowp[DOT ? 4 : 1][kChunk], colp[DOT ? 4 : 1][kChunk], dots[DOT ? NW : 1][kChunk];
+    __shared__ int wild[2];
+    __shared__ float rowp[DOT ? 4 : 1][kChunk], colp[DOT ? 4 : 1][kChunk], dots[DOT ? NW / RG : 1][kChunk];
 
     const DecayRun &A = R.run[blockIdx.y];
     const bool pairs = MODE == DECAY_DOT && A.pairs;
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-    const int n = lane % 16, q = lane / 16, c0 = 16 * wave;
+    const int n = lane % 16, q = lane / 16, group = wave / RG, rg = wave % RG, c0 = 16 * CT * group;
+    auto row_tile = [&](int m) { return RG == 1 ? m : rg ? 1 + m : 3 * m; };  // (pairs of tiles with equally long sums)
     const int p = blockIdx.x / A.heads, h = blockIdx.x % A.heads, dir = A.dir;
     const int bad = any_bad(A.bad), olo = A.offsets[0], ohi = A.offsets[A.n_seqs];
     const Spans::Border b0 = A.spans.border(p), b1 = A.spans.border(p + 1);
@@ -342,17 +368,36 @@ __global__ __launch_bounds__(4 * DV, DK * DV <= 64 * 64 && DV == 64 ? 3 : 2) voi
     // both directions have the same ones (db's two halves are split by chunks).
     const int chunks = (hi - lo + kChunk - 1) / kChunk;
 
-    o_f32x4 S[ST];
+    o_f32x4 S[CT][ST];
+    auto clear_state = [&] {
 #pragma unroll
-    for (int m = 0; m < ST; ++m) S[m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < CT; ++j)
+#pragma unroll
+            for (int m = 0; m < ST; ++m) S[j][m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
+    };
+    clear_state();
     bool have = false;  // the state is that of the sequence that goes on
     auto load_state = [&](const float *s) {
-        const int step = A.turned ? 1 : DV;
+        const int step = A.turned ? 1 : DV, next = A.turned ? 16 * DK : 16;
         const float *e = s + (A.turned ? (c0 + n) * DK + 4 * q : 4 * q * DV + c0 + n);
 #pragma unroll
-        for (int m = 0; m < ST; ++m)
+        for (int j = 0; j < CT; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) S[m][i] = e[(16 * m + i) * step];
+            for (int m = 0; m < ST; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) S[j][m][i] = e[(16 * m + i) * step + j * next];
+    };
+    auto save_state = [&](float *s, bool turned, float d) {
+        const int step = turned ? 1 : DV, next = turned ? 16 * DK : 16;
+        float *e = s + (turned ? (c0 + n) * DK + 4 * q : 4 * q * DV + c0 + n);
+        if (rg == 0) {
+#pragma unroll
+            for (int j = 0; j < CT; ++j)
+#pragma unroll
+                for (int m = 0; m < ST; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) e[(16 * m + i) * step + j * next] = S[j][m][i] * d;
+        }
     };
     if (OUT && cut_in) {
         load_state(A.local + ((long long)(p - dir) * A.heads + h) * (DK * DV));
@@ -367,7 +412,7 @@ __global__ __launch_bounds__(4 * DV, DK * DV <= 64 * 64 && DV == 64 ? 3 : 2) voi
     const char *bk = (const char *)A.k + ((long long)lo * A.ks + h / A.kg * DK) * ES;
     const char *bv = (const char *)A.v + ((long long)lo * A.vs + h / A.vg * DV) * ES;
     if (DOT) bx = (const char *)A.x + ((long long)lo * A.xs + h / A.xg * DV) * ES;
-    auto chunk_rows = [&](int at) { return hi - lo - at < kChunk ? hi - lo - at : kChunk; };
+    auto chunk_rows = [&](int at) { return at < 0 || at >= hi - lo ? 0 : hi - lo - at < kChunk ? hi - lo - at : kChunk; };
     auto chunk_at = [&](int c) { return (dir > 0 ? c : chunks - 1 - c) * kChunk; };  // the c-th on the way: its first row in memory, from lo
     auto fetch = [&](int c) {
         const int at = chunk_at(c), rows = chunk_rows(at);
@@ -381,8 +426,8 @@ __global__ __launch_bounds__(4 * DV, DK * DV <= 64 * 64 && DV == 64 ? 3 : 2) voi
     float next_g = 0.0f;
     double total = 0.0;
     auto fetch_rows = [&](int c) {
-        const int at = chunk_at(c), rows = chunk_rows(at), i = lane < rows ? lane : rows - 1;
-        const int r = lo + at + (dir > 0 ? i : rows - 1 - i);
+        const int at = chunk_at(c), rows = chunk_rows(at), i = lane < rows ? lane : 0;
+        const int r = rows ? lo + at + (dir > 0 ? i : rows - 1 - i) : lo;
         next_seq = A.spans.info[r];
         int rg = A.shift ? r - dir : r;  // (where that is another sequence's it is not used)
         rg = rg < olo ? olo : rg >= ohi ? ohi - 1 : rg;
@@ -409,24 +454,34 @@ __global__ __launch_bounds__(4 * DV, DK * DV <= 64 * 64 && DV == 64 ? 3 : 2) voi
         W.seg[i] = (f < 0 ? 0 : f + 1) | (i < rows ? e + 1 : i + 1) << 8 | (l <= rows - 1 ? 1 << 16 : 0);
         if (!OUT) total += __shfl(b, rows - 1);
     };
-    fetch(0);
-    if (wave == NW - 1) {
-        fetch_rows(0);
-        put_rows(rows_of[0], 0);
-        if (chunks > 1) fetch_rows(1);
-    }
-    if (OUT)  // the weights above the diagonal that share a fragment with some below
-        for (int i = tid; i < kChunk * LP * (int)sizeof(ME) / 4; i += NT) ((unsigned *)Ps)[i] = 0;
-
-    for (int c = 0; c < chunks; ++c) {
-        const int at = chunk_at(c), rows = chunk_rows(at);
-        const ChunkRows &W = rows_of[c & 1];
+    // What a chunk's loads bring goes to LDS when the chunk before is done with it.  The registers in between are this
+    // chunk's own (carried around the loop they would be copied at its end, and waited for there).
+    auto put = [&](int c) {
+        const int rows = chunk_rows(chunk_at(c));
         if (OUT) tq.store(Qs, rows, dir, tid);
         tk.store(Ks, rows, dir, tid);
         tv.store(Vs, rows, dir, tid);
         if (DOT) tx.store(Xs, rows, dir, tid);
-        const bool slow = __syncthreads_or(tk.infinite() || tv.infinite());
-        if (c + 1 < chunks) fetch(c + 1);
+        if (tk.infinite() || tv.infinite()) wild[c & 1] = 1;
+    };
+    fetch(0);
+    if (tid < 2) wild[tid] = 0;
+    if (wave == NW - 1) {
+        fetch_rows(0);
+        put_rows(rows_of[0], 0);
+    }
+    if (OUT)  // the weights above the diagonal that share a fragment with some below
+        for (int i = tid; i < kChunk * LP * (int)sizeof(ME) / 4; i += NT) ((unsigned *)Ps)[i] = 0;
+    __syncthreads();
+    put(0);
+    __syncthreads();
+
+    for (int c = 0; c < chunks; ++c) {
+        const int at = chunk_at(c), rows = chunk_rows(at);
+        const ChunkRows &W = rows_of[c & 1];
+        const bool slow = __builtin_amdgcn_readfirstlane(wild[c & 1]);
+        fetch(c + 1);
+        if (wave == NW - 1) fetch_rows(c + 1);
 
         if (OUT) {
             // weights: tile (s tile ms, t tile mt), transposed, so that four consecutive s of a row t land in a lane
@@ -439,9 +494,10 @@ __global__ __launch_bounds__(4 * DV, DK * DV <= 64 * 64 && DV == 64 ? 3 : 2) voi
                 typedef __attribute__((ext_vector_type(4))) ME V4;
                 o_f32x4 a = {0.f, 0.f, 0.f, 0.f};
                 if (!apart) {
-#pragma unroll
-                    for (int k0 = 0; k0 < DK; k0 += KM)
-                        a = M::mma(M::along(Ks, LK, 16 * ms + n, k0, q), M::along(Qs, LK, 16 * mt + n, k0, q), a);
+                    struct Two { F k, q; };
+                    in_turn<DK / KM, (DK / KM < 4 ? DK / KM + 1 : 4)>(
+                        [&](int i) { return Two{M::along(Ks, LK, 16 * ms + n, i * KM, q), M::along(Qs, LK, 16 * mt + n, i * KM, q)}; },
+                        [&](int, Two f) { a = M::mma(f.k, f.q, a); });
                     const float th = W.bh[t], tl = W.bl[t];
                     const o_f32x4 sh = *(const o_f32x4 *)&W.bh[s], sl = *(const o_f32x4 *)&W.bl[s];
 #pragma unroll
@@ -478,9 +534,11 @@ __global__ __launch_bounds__(4 * DV, DK * DV <= 64 * 64 && DV == 64 ? 3 : 2) voi
             __syncthreads();
         }
 
-        o_f32x4 o[4];
+        o_f32x4 o[CT][TM];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) o[m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < CT; ++j)
+#pragma unroll
+            for (int m = 0; m < TM; ++m) o[j][m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
         // The chunk's sequences, one after the other: what their state adds to their rows, and the state after them.  Those
         // that are whole in the chunk have none, unless states come in or go out.
 #pragma unroll 1
@@ -495,79 +553,94 @@ __global__ __launch_bounds__(4 * DV, DK * DV <= 64 * 64 && DV == 64 ? 3 : 2) voi
                 if (have) load_state(A.s0 + ((long long)seq * A.heads + h) * (DK * DV));
             }
             if (OUT && have) {
-                o_f32x4 z[4];
+                o_f32x4 z[CT][TM];
 #pragma unroll
-                for (int m = 0; m < 4; ++m) z[m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int j = 0; j < CT; ++j)
 #pragma unroll
-                for (int k = 0; k < DK / KM; ++k) {
-                    float x[4 * M::TILES];
+                    for (int m = 0; m < TM; ++m) z[j][m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
+                F sp[CT][NS];
+                in_turn<DK / KM * TM, 4>([&](int i) { return M::along_state(Qs, LK, 16 * row_tile(i % TM) + n, i / TM * KM, q); },
+                                         [&](int i, F f) {
+                                             const int k = i / TM, m = i % TM;
+                                             if (m == 0) {
 #pragma unroll
-                    for (int i = 0; i < 4 * M::TILES; ++i) x[i] = S[k * M::TILES + i / 4][i % 4];
-                    F sp[NS];
-                    M::template split<NS>(x, sp);
+                                                 for (int j = 0; j < CT; ++j) {
+                                                     float x[4 * M::TILES];
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        if (16 * m + 16 <= a || 16 * m >= b) continue;
-                        const F f = M::along_state(Qs, LK, 16 * m + n, k * KM, q);
+                                                     for (int e = 0; e < 4 * M::TILES; ++e) x[e] = S[j][k * M::TILES + e / 4][e % 4];
+                                                     M::template split<NS>(x, sp[j]);
+                                                 }
+                                             }
 #pragma unroll
-                        for (int j = NS - 1; j >= 0; --j) z[m] = M::mma(sp[j], f, z[m]);
-                    }
-                }
+                                             for (int e = NS - 1; e >= 0; --e)
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    const int t = 16 * m + n;
+                                                 for (int j = 0; j < CT; ++j) z[j][m] = M::mma(sp[j][e], f, z[j][m]);
+                                         });
+#pragma unroll
+                for (int m = 0; m < TM; ++m) {
+                    const int t = 16 * row_tile(m) + n;
                     const float f = W.in[t];
+                    const bool on = t >= a && t < b;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[m][i] = t >= a && t < b ? z[m][i] * f : o[m][i];
+                    for (int j = 0; j < CT; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[j][m][i] = on ? z[j][m][i] * f : o[j][m][i];
                 }
             }
             if (!ends || A.sf) {
-                const float d = W.decay[b - 1];
+                if (have) {
+                    const float d = W.decay[b - 1];
 #pragma unroll
-                for (int m = 0; m < ST; ++m) S[m] = have ? S[m] * d : o_f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int j = 0; j < CT; ++j)
+#pragma unroll
+                        for (int m = 0; m < ST; ++m) S[j][m] *= d;
+                } else {
+                    clear_state();
+                }
                 if (!slow) {
 #pragma unroll
                     for (int k = 0; k < NB; ++k) {
                         if (k * KM + KM <= a || k * KM >= b) continue;
-                        const F v = M::down(Vs, LV, k * KM, c0, n, q);
-                        float x[KM / 4];
+                        F vp[CT][NU];
+                        float w[KM / 4];
 #pragma unroll
-                        for (int i = 0; i < KM / 4; i += 4) {
-                            const int s = k * KM + KM / 4 * q + i;
-                            const o_f32x4 w = *(const o_f32x4 *)&W.to[s];
+                        for (int i = 0; i < KM / 4; i += 4) *(o_f32x4 *)&w[i] = *(const o_f32x4 *)&W.to[k * KM + KM / 4 * q + i];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) x[i + j] = s + j >= a && s + j < b ? (float)v[i + j] * w[j] : 0.0f;
+                        for (int j = 0; j < CT; ++j) {
+                            const F v = M::down(Vs, LV, k * KM, c0 + 16 * j, n, q);
+                            float x[KM / 4];
+#pragma unroll
+                            for (int i = 0; i < KM / 4; ++i) {
+                                const int s = k * KM + KM / 4 * q + i;
+                                x[i] = s >= a && s < b ? (float)v[i] * w[i] : 0.0f;
+                            }
+                            M::template split<NU>(x, vp[j]);
                         }
-                        F vp[NU];
-                        M::template split<NU>(x, vp);
+                        in_turn<ST, 3>([&](int m) { return M::down(Ks, LK, k * KM, 16 * m, n, q); },
+                                       [&](int m, F kf) {
 #pragma unroll
-                        for (int m = 0; m < ST; ++m) {
-                            const F kf = M::down(Ks, LK, k * KM, 16 * m, n, q);
+                                           for (int i = NU - 1; i >= 0; --i)
 #pragma unroll
-                            for (int j = NU - 1; j >= 0; --j) S[m] = M::mma(kf, vp[j], S[m]);
-                        }
+                                               for (int j = 0; j < CT; ++j) S[j][m] = M::mma(kf, vp[j][i], S[j][m]);
+                                       });
                     }
                 } else {
 #pragma unroll 1
-                    for (int s = a; s < b; ++s) {
-                        const float v = (float)Vs[s * LV + c0 + n] * W.to[s];
+                    for (int s = a; s < b; ++s)
 #pragma unroll
-                        for (int m = 0; m < ST; ++m)
+                        for (int j = 0; j < CT; ++j) {
+                            const float v = (float)Vs[s * LV + c0 + 16 * j + n] * W.to[s];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) S[m][i] += (float)Ks[s * LK + 16 * m + 4 * q + i] * v;
-                    }
+                            for (int m = 0; m < ST; ++m)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) S[j][m][i] += (float)Ks[s * LK + 16 * m + 4 * q + i] * v;
+                        }
                 }
                 have = true;
                 if (ends && A.sf) {
-                    float *s = A.sf + ((long long)seq * A.heads + h) * (DK * DV);
                     float d = 1.0f;
                     if (A.sf_decay) d = expf(log_decay_of(A, lo + at + (dir > 0 ? b - 1 : rows - b), h));
-                    const int step = A.turned ? 1 : DV;
-                    float *e = s + (A.turned ? (c0 + n) * DK + 4 * q : 4 * q * DV + c0 + n);
-#pragma unroll
-                    for (int m = 0; m < ST; ++m)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) e[(16 * m + i) * step] = S[m][i] * d;
+                    save_state(A.sf + ((long long)seq * A.heads + h) * (DK * DV), A.turned, d);
                 }
             }
             a = b;
@@ -579,58 +652,77 @@ __global__ __launch_bounds__(4 * DV, DK * DV <= 64 * 64 && DV == 64 ? 3 : 2) voi
         if (OUT) {
             if (DOT) {
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
+                for (int m = 0; m < TM; ++m) {
                     float z = 0.0f;
                     typedef __attribute__((ext_vector_type(4))) ME V4;
-                    const o_f32x4 x = __builtin_convertvector(*(const V4 *)(Xs + (16 * m + n) * LV + c0 + 4 * q), o_f32x4);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) z += o[m][i] * x[i];
+                    for (int j = 0; j < CT; ++j) {
+                        const o_f32x4 x = __builtin_convertvector(*(const V4 *)(Xs + (16 * row_tile(m) + n) * LV + c0 + 16 * j + 4 * q), o_f32x4);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) z += o[j][m][i] * x[i];
+                    }
                     z += __shfl_xor(z, 16);
                     z += __shfl_xor(z, 32);
-                    if (q == 0) dots[wave][16 * m + n] = z;
+                    if (q == 0) dots[group][16 * row_tile(m) + n] = z;
                 }
             }
             if (!slow) {
+                F v[CT];
+                in_turn<NB * TM, 4>(
+                    [&](int i) {
+                        F f = {};
+                        if (i / TM * KM <= 16 * row_tile(i % TM)) f = M::along(Ps, LP, 16 * row_tile(i % TM) + n, i / TM * KM, q);
+                        return f;
+                    },
+                    [&](int i, F f) {
+                        const int k = i / TM, m = i % TM;
+                        if (m == 0) {
 #pragma unroll
-                for (int k = 0; k < NB; ++k) {
-                    const F v = M::down(Vs, LV, k * KM, c0, n, q);
+                            for (int j = 0; j < CT; ++j) v[j] = M::down(Vs, LV, k * KM, c0 + 16 * j, n, q);
+                        }
+                        if (k * KM <= 16 * row_tile(m)) {
 #pragma unroll
-                    for (int m = 0; m < 4; ++m)
-                        if (k * KM <= 16 * m) o[m] = M::mma(v, M::along(Ps, LP, 16 * m + n, k * KM, q), o[m]);
-                }
+                            for (int j = 0; j < CT; ++j) o[j][m] = M::mma(v[j], f, o[j][m]);
+                        }
+                    });
             } else {
                 // an infinite or NaN k or v: only the products that the definition has
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    const int t = 16 * m + n, f = seg_first(W.seg[t]);
+                for (int m = 0; m < TM; ++m) {
+                    const int t = 16 * row_tile(m) + n, f = seg_first(W.seg[t]);
                     for (int s = f > 0 ? f : 0; s <= t; ++s)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) o[m][i] += (float)Ps[t * LP + s] * (float)Vs[s * LV + c0 + 4 * q + i];
+                        for (int j = 0; j < CT; ++j)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                o[j][m][i] += (float)Ps[t * LP + s] * (float)Vs[s * LV + c0 + 16 * j + 4 * q + i];
                 }
             }
             // (the chunk's first row is a scalar; 64 rows of a stride fit in 32 bits)
             const int es = A.out_f32 ? 4 : ES;
             char *ob = (char *)A.out + ((long long)(lo + at) * A.os + h * DV + c0) * es;
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                const int t = 16 * m + n;
+            for (int m = 0; m < TM; ++m) {
+                const int t = 16 * row_tile(m) + n;
                 if (t < rows) {
                     char *to = ob + (unsigned)((dir > 0 ? t : rows - 1 - t) * (int)A.os + 4 * q) * (unsigned)es;
-                    if (A.out_f32) *(o_f32x4 *)to = o[m];
-                    else store4<T>((typename T::E *)to, o[m]);
+#pragma unroll
+                    for (int j = 0; j < CT; ++j) {
+                        if (A.out_f32) *(o_f32x4 *)(to + 64 * j) = o[j][m];
+                        else store4<T>((typename T::E *)(to + 16 * j * ES), o[j][m]);
+                    }
                 }
             }
         }
-        if (wave == NW - 1 && c + 1 < chunks) {
-            put_rows(rows_of[(c + 1) & 1], c + 1);
-            if (c + 2 < chunks) fetch_rows(c + 2);
-        }
+        if (wave == NW - 1 && c + 1 < chunks) put_rows(rows_of[(c + 1) & 1], c + 1);
         __syncthreads();
+        if (tid == 0) wild[c & 1] = 0;
+        put(c + 1);
         if (DOT && wave == 0) {
             const int t = lane;
             if (t < rows) {
                 float z = 0.0f;
-                for (int w = 0; w < NW; ++w) z += dots[w][t];
+                for (int w = 0; w < NW / RG; ++w) z += dots[w][t];
                 if (pairs)
                     for (int m = 0; m < 4; ++m) {
                         if (m <= t / 16) z += rowp[m][t];
@@ -639,13 +731,10 @@ __global__ __launch_bounds__(4 * DV, DK * DV <= 64 * 64 && DV == 64 ? 3 : 2) voi
                 A.db[(long long)(lo + at + (dir > 0 ? t : rows - 1 - t)) * A.heads + h] = z;
             }
         }
+        __syncthreads();
     }
     if (!OUT) {
-        float *s = A.local + ((long long)p * A.heads + h) * (DK * DV) + 4 * q * DV + c0 + n;
-#pragma unroll
-        for (int m = 0; m < ST; ++m)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[(16 * m + i) * DV] = S[m][i];
+        save_state(A.local + ((long long)p * A.heads + h) * (DK * DV), false, 1.0f);
         if (wave == NW - 1 && lane == 0) A.mult[(long long)p * A.heads + h] = whole ? exp2_of(total) : 0.0f;
     }
 }
@@ -714,40 +803,63 @@ __global__ __launch_bounds__(256) void tf_decay_index_kernel(const int32_t *__re
     }
 }
 
-// The states at the spans' ends from the spans' own contributions, in order along each cut sequence: a workgroup has
-// 1024 values of the states of one sequence's cuts and head, from its first.  The next spans' contributions are read while
-// the sum is on its way.
+// The states at the spans' ends from the spans' own contributions, in order along each cut sequence.  A wave has 256
+// values of one head's states and every kChains-th span; where that is a sequence's first cut it follows the sequence, the
+// next spans' contributions on their way while it adds (each sum stays for the span that follows).
+constexpr int kChains = 16;
 __global__ __launch_bounds__(256) void tf_decay_chain_kernel(DecayRuns R, int size) {
     const DecayRun &A = R.run[blockIdx.z];
     if (any_bad(A.bad)) return;
-    const int heads = A.heads, spans = A.spans.n, dir = A.dir;
-    const int p = blockIdx.x / heads, h = blockIdx.x % heads, e = (blockIdx.y * 256 + threadIdx.x) * 4;
-    if (A.kind[p] != 1) return;  // a sequence's first cut
-    int cuts = 0;
-    for (int i = p + dir; i >= 0 && i < spans; i += 64 * dir) {  // how many spans it goes on through whole
-        const int j = i + dir * (int)(threadIdx.x % 64);
-        const unsigned long long on = __ballot(j >= 0 && j < spans && A.kind[j < 0 ? 0 : j < spans ? j : spans - 1] == 2);
-        const int run = ~on ? __builtin_ctzll(~on) : 64;
-        cuts += run;
-        if (run < 64) break;
-    }
+    const int heads = A.heads, spans = A.spans.n, dir = A.dir, lane = threadIdx.x % 64;
+    const int h = blockIdx.x / (kChains / 4), e = (blockIdx.y * 64 + lane) * 4;
     const long long step = (long long)dir * heads * size;
-    float *l = A.local + ((long long)p * heads + h) * size + e;
-    const float *m = A.mult + (long long)p * heads + h;
-    o_f32x4 s = *(const o_f32x4 *)l;
-    constexpr int AHEAD = 8;
-    for (int i = 0; i < cuts; i += AHEAD) {
-        o_f32x4 x[AHEAD];
-        float w[AHEAD];
-#pragma unroll
-        for (int j = 0; j < AHEAD; ++j)
-            if (i + j < cuts) x[j] = *(const o_f32x4 *)(l + (i + j + 1) * step), w[j] = m[(long long)(i + j + 1) * dir * heads];
-#pragma unroll
-        for (int j = 0; j < AHEAD; ++j)
-            if (i + j < cuts) {
-                s = x[j] + s * w[j];
-                *(o_f32x4 *)(l + (i + j + 1) * step) = s;
+    for (int first = blockIdx.x % (kChains / 4) * 4 + threadIdx.x / 64; first < spans; first += kChains * 64) {
+        const int mine = first + kChains * lane;
+        unsigned long long starts = __ballot(mine < spans && A.kind[mine < spans ? mine : 0] == 1);
+        while (starts) {
+            const int p = first + kChains * __builtin_ctzll(starts);
+            starts &= starts - 1;
+            int cuts = 0;
+            for (int i = p + dir; i >= 0 && i < spans; i += 64 * dir) {  // how many spans it goes on through whole
+                const int j = i + dir * lane;
+                const bool in = j >= 0 && j < spans;
+                const unsigned long long on = __ballot(in && A.kind[in ? j : 0] == 2);
+                const int run = ~on ? __builtin_ctzll(~on) : 64;
+                cuts += run;
+                if (run < 64) break;
             }
+            if (cuts == 0) continue;
+            float *l = A.local + ((long long)p * heads + h) * size + e;
+            const float *m = A.mult + (long long)p * heads + h;
+            o_f32x4 s = *(const o_f32x4 *)l;
+            // Batches in turn, so that a batch's loads are waited for behind the next one's and not behind its stores (stores
+            // under a branch would be waited for one by one: behind the end the last sum is stored again).
+            constexpr int BATCH = 8;
+            o_f32x4 x[2][BATCH];
+            float w[2][BATCH];
+            auto load = [&](int b, int i) {
+#pragma unroll
+                for (int j = 0; j < BATCH; ++j) {
+                    const int k = i + j < cuts ? i + j + 1 : cuts;
+                    x[b][j] = *(const o_f32x4 *)(l + k * step), w[b][j] = m[(long long)k * dir * heads];
+                }
+            };
+            auto add = [&](int b, int i) {
+#pragma unroll
+                for (int j = 0; j < BATCH; ++j) {
+                    const bool in = i + j < cuts;
+                    if (in) s = x[b][j] + s * w[b][j];
+                    *(o_f32x4 *)(l + (in ? i + j + 1 : cuts) * step) = s;
+                }
+            };
+            load(0, 0);
+            for (int i = 0; i < cuts; i += 2 * BATCH) {
+                load(1, i + BATCH);
+                add(0, i);
+                load(0, i + 2 * BATCH);
+                add(1, i + BATCH);
+            }
+        }
     }
 }
 
@@ -1006,7 +1118,7 @@ Plan decay_plan(const tf_decay_config *c, int64_t n_rows, int64_t n_seqs, bool b
 }
 
 template <class T, int DK, int DV> void span_mode(const DecayRuns &R, int runs, int mode, hipStream_t s) {
-    const dim3 grid((unsigned)(R.run[0].spans.n * R.run[0].heads), runs), block(4 * DV);
+    const dim3 grid((unsigned)(R.run[0].spans.n * R.run[0].heads), runs), block(span_threads(DV));
     switch (mode) {
         case DECAY_STATE: hipLaunchKernelGGL((tf_decay_span_kernel<T, DK, DV, DECAY_STATE>), grid, block, 0, s, R); break;
         case DECAY_OUT: hipLaunchKernelGGL((tf_decay_span_kernel<T, DK, DV, DECAY_OUT>), grid, block, 0, s, R); break;
@@ -1034,7 +1146,7 @@ void chain_run(int elem, DecayRuns R, int runs, int dk, int dv, hipStream_t s) {
     if (A.spans.n < 2) return;
     for (int i = 0; i < runs; ++i) R.run[i].sf = nullptr, R.run[i].turned = 0;
     span_run(elem, R, runs, dk, dv, DECAY_STATE, s);
-    hipLaunchKernelGGL(tf_decay_chain_kernel, dim3((unsigned)(A.spans.n * A.heads), (unsigned)(dk * dv / 1024), runs), dim3(256), 0, s, R,
+    hipLaunchKernelGGL(tf_decay_chain_kernel, dim3((unsigned)(kChains / 4 * A.heads), (unsigned)(dk * dv / 256), runs), dim3(256), 0, s, R,
                        dk * dv);
 }
 void index_run(const int32_t *offsets, int n_seqs, int64_t n_rows, const Plan &p, int32_t *flags, hipStream_t s) {

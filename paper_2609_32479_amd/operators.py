@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import math
 
 import torch
@@ -78,23 +79,46 @@ def _check(status: int, what: str):
     check(status, what)
 
 
-@contextlib.contextmanager
-def _on(tensor: torch.Tensor, stream):
-    """The tensor's device, with ``stream`` as its current stream; yields the stream's handle."""
-    with torch.cuda.device(tensor.device):
+@functools.lru_cache(maxsize=256)
+def _config(kind, *fields):
+    """A configuration of these plain values (read only: the library takes it by pointer)."""
+    return kind(*fields)
+
+
+class _On:
+    """The tensor's device, with ``stream`` as its current stream; entering gives the stream's handle."""
+    __slots__ = ("stack", "handle")
+
+    def __init__(self, tensor: torch.Tensor, stream):
+        index = tensor.get_device()
+        if stream is None and index == torch.cuda.current_device():  # nothing to switch
+            self.stack, self.handle = None, torch._C._cuda_getCurrentRawStream(index)
+            return
+        self.stack = contextlib.ExitStack()
+        self.stack.enter_context(torch.cuda.device(index))
         if stream is None:
-            yield int(torch.cuda.current_stream().cuda_stream)
-        else:
-            if not hasattr(stream, "cuda_stream"):
-                stream = torch.cuda.ExternalStream(int(stream))
-            with torch.cuda.stream(stream):
-                yield int(stream.cuda_stream)
+            self.handle = int(torch.cuda.current_stream().cuda_stream)
+            return
+        if not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream))
+        self.stack.enter_context(torch.cuda.stream(stream))
+        self.handle = int(stream.cuda_stream)
+
+    def __enter__(self) -> int:
+        return self.handle
+
+    def __exit__(self, *exc):
+        if self.stack is not None:
+            self.stack.close()
+
+
+_on = _On
 
 
 def _same(name: str, x, like: torch.Tensor, dtype=None):
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
-    if x.device != like.device:
+    if x.get_device() != like.get_device():
         raise ValueError(f"{name} is on {x.device}, the others on {like.device}")
     if dtype is not None and x.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, not {x.dtype}")
@@ -111,18 +135,23 @@ def _elem(x) -> int:
 def _rows3(name: str, x: torch.Tensor, like: torch.Tensor, rows=None, heads=None, width=None) -> int:
     """Check a [rows, heads, width] tensor whose rows are contiguous; returns its row stride."""
     _same(name, x, like, like.dtype)
-    if x.dim() != 3 or (rows is not None and x.shape[0] != rows) or (heads is not None and x.shape[1] != heads) or \
-            (width is not None and x.shape[2] != width):
+    shape = x.shape
+    if len(shape) != 3 or (rows is not None and shape[0] != rows) or (heads is not None and shape[1] != heads) or \
+            (width is not None and shape[2] != width):
         want = ", ".join("?" if v is None else str(v) for v in (rows, heads, width))
-        raise ValueError(f"{name} must have shape [{want}], not {list(x.shape)}")
-    if (x.shape[2] > 1 and x.stride(2) != 1) or (x.shape[1] > 1 and x.stride(1) != x.shape[2]):
+        raise ValueError(f"{name} must have shape [{want}], not {list(shape)}")
+    r, h, w = shape
+    n = h * w
+    if x.is_contiguous():
+        return n
+    sr, sh, sw = x.stride()
+    if (w > 1 and sw != 1) or (h > 1 and sh != w):
         raise ValueError(f"{name}'s rows [heads, width] must be contiguous")
-    n = x.shape[1] * x.shape[2]
-    if x.shape[0] <= 1:
+    if r <= 1:
         return n  # (one row: any stride)
-    if x.stride(0) < n:
+    if sr < n:
         raise ValueError(f"{name}'s rows overlap")
-    return x.stride(0)
+    return sr
 
 
 def _new(name: str, x, like: torch.Tensor, shape, dtype) -> torch.Tensor:
@@ -138,7 +167,7 @@ def _new(name: str, x, like: torch.Tensor, shape, dtype) -> torch.Tensor:
 def _rows_out(name: str, x, like: torch.Tensor, shape):
     """The output rows (new, or the caller's, which may be strided) and their stride."""
     if x is None:
-        x = torch.empty(shape, dtype=like.dtype, device=like.device)
+        return torch.empty(shape, dtype=like.dtype, device=like.device), shape[1] * shape[2]
     return x, _rows3(name, x, like, *shape)
 
 
@@ -203,7 +232,7 @@ def _decay_inputs(q, k, v, scale, reverse):
     heads, dv = v.shape[1], v.shape[2]
     strides = (_rows3("q", q, q), _rows3("k", k, q, rows, qk_heads, dk), _rows3("v", v, q, rows))
     scale = dk ** -0.5 if scale is None else float(scale)
-    return DecayConfig(elem, heads, qk_heads, dk, dv, int(bool(reverse)), scale), strides
+    return _config(DecayConfig, elem, heads, qk_heads, dk, dv, int(bool(reverse)), scale), strides
 
 
 def decay_attention(q, k, v, log_decay, offsets, scale=None, reverse=False, initial_state=None, return_state=False,
@@ -310,7 +339,7 @@ def _norm_inputs(q, k, q_gain, k_gain, offsets, positions, rotary_dim, base, int
     rot = d if rotary_dim is None else int(rotary_dim)
     if not math.isfinite(float(base)):
         raise ValueError("base must be finite")
-    return QKNormConfig(elem, hq, k.shape[1], d, rot, int(bool(interleaved)), float(eps), float(base)), qs, ks, n
+    return _config(QKNormConfig, elem, hq, k.shape[1], d, rot, int(bool(interleaved)), float(eps), float(base)), qs, ks, n
 
 
 def qk_norm_rotate(q, k, q_gain, k_gain, offsets=None, positions=None, rotary_dim=None, base=10000.0, interleaved=False,
@@ -382,7 +411,7 @@ def _gated_inputs(x, w_gate, w_up, activation):
     wu = _matrix("w_up", w_up, x, w_gate.shape[0], x.shape[1])
     if ws != wu:
         raise ValueError("w_gate and w_up must have the same row stride")
-    return GatedConfig(elem, x.shape[1], w_gate.shape[0], _ACTIVATIONS[activation]), xs, ws
+    return _config(GatedConfig, elem, x.shape[1], w_gate.shape[0], _ACTIVATIONS[activation]), xs, ws
 
 
 def gated_ffn(x, w_gate, w_up, activation="silu", out=None, stream=None):
