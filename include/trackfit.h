@@ -529,8 +529,10 @@ tf_status tf_decay_attention_step(const tf_decay_config *cfg, const void *q, int
  *   (lo, hi) -> (lo cos a - hi sin a, lo sin a + hi cos a),  a = position base^(-2 j / rotary_dim)
  * for pairs j < rotary_dim / 2: values j and j + rotary_dim / 2, or (interleaved)
  * 2 j and 2 j + 1.  Values from rotary_dim on are only normalised.
- * Sums and products in fp32, angles in fp64, one rounding at the store.
- * Supported: head_dim 32, 64, 128 or 256, rotary_dim a multiple of 16 up to it.
+ * Sums and products in fp32, angles in fp64, one rounding at the store (16-bit
+ * types: sines and cosines good to 2^-20).
+ * Supported: head_dim 32, 64, 128 or 256, rotary_dim a multiple of 16 up to it, up to
+ * 1024 heads of each, row strides up to 2^22.
  */
 typedef struct {
     int32_t elem;        /* tf_elem of q, k, the outputs and their gradients */

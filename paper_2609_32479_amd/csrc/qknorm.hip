@@ -20,6 +20,7 @@
 #include "ops.h"
 
 #include <cmath>
+#include <initializer_list>
 
 namespace {
 
@@ -43,6 +44,7 @@ struct NormArgs {
     long long n_rows;
     const int32_t *positions, *offsets;
     int n_seqs, rot, tile;  // rotated values; rows of a tile
+    unsigned per_head[2], per_pair;  // 2^32 over the heads, the pairs (rounded down)
     float eps;
     float *parts;  // backward: [workgroups][2][D]
 };
@@ -80,6 +82,12 @@ __device__ __forceinline__ void norm_store(typename T::E *p, int l, int rot, con
     store8<T>(p + b, y);
 }
 
+// a / b, with r = 2^32 / b rounded down (or 2^32 - 1): at most one too small.
+__device__ __forceinline__ int over(int a, int b, unsigned r) {
+    const int d = (int)__umulhi((unsigned)a, r);
+    return a - d * b >= b ? d + 1 : d;
+}
+
 template <int L> __device__ __forceinline__ float head_sum(float s) {
 #pragma unroll
     for (int m = 1; m < L; m *= 2) s += __shfl_xor(s, m);
@@ -90,20 +98,18 @@ template <typename T, int D, bool PAIRED, bool BACK>
 __global__ __launch_bounds__(kNormBlock) void tf_qk_norm_kernel(NormArgs A, Turns turns) {
     constexpr int L = D / 16;  // lanes of a head
     typedef typename T::E E;
-    __shared__ float cs[2 * kNormAngles];  // [row][cos, sin][pair]
+    __shared__ __attribute__((aligned(16))) float cs[2 * kNormAngles];  // [row][cos, sin][pair]
     __shared__ double at[kNormRows];  // positions
     __shared__ int live[kNormRows];
     const int tid = threadIdx.x, l = tid % L;
-    const int pairs = A.rot / 2, heads = A.heads[0] + A.heads[1];
+    const int pairs = A.rot / 2;
     const bool turned = 16 * l < A.rot;
 
-    float gain[2][16], acc[2][16];
+    float acc[2][16];
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        norm_load<ElemF32, PAIRED>(A.gain[w], l, A.rot, gain[w]);
+    for (int w = 0; w < 2; ++w)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[w][i] = 0.0f;
-    }
     long long first = 0, last = A.n_rows;
     if (A.offsets) {
         const long long o = A.offsets[0], e = A.offsets[A.n_seqs];
@@ -129,69 +135,82 @@ __global__ __launch_bounds__(kNormBlock) void tf_qk_norm_kernel(NormArgs A, Turn
         }
         __syncthreads();
         for (int i = tid; i < rows * pairs; i += kNormBlock) {
-            const int r = i / pairs, j = i - r * pairs;
+            const int r = over(i, pairs, A.per_pair), j = i - r * pairs;
             double a = at[r] * turns.f[j];
             a -= rint(a);
             float sn, co;
-            sincospif(2.0f * (float)a, &sn, &co);
+            if constexpr (sizeof(E) == 4) {
+                sincospif(2.0f * (float)a, &sn, &co);
+            } else {  // the hardware's, of turns: within 2^-20, below the outputs' rounding
+                sn = __builtin_amdgcn_sinf((float)a), co = __builtin_amdgcn_cosf((float)a);
+            }
             cs[2 * pairs * r + j] = co, cs[2 * pairs * r + pairs + j] = sn;
         }
         __syncthreads();
-        const int items = rows * heads * L;
-        for (int it = tid; it < items; it += kNormBlock) {
-            const int rh = it / L, r = rh / heads, h = rh - r * heads;
-            const bool isk = h >= A.heads[0];
-            const int w = isk ? 1 : 0, hh = isk ? h - A.heads[0] : h;
-            if (!live[r]) continue;  // the lanes of a head agree
-            float v[16], c[8], s[8];
-            norm_load<T, PAIRED>((const E *)A.x[w] + (r0 + r) * A.xs[w] + (long long)hh * D, l, A.rot, v);
-            if (turned) {
+        // queries, then keys
 #pragma unroll
-                for (int i = 0; i < 8; ++i) c[i] = cs[2 * pairs * r + 8 * l + i], s[i] = cs[2 * pairs * r + pairs + 8 * l + i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) c[i] = 1.0f, s[i] = 0.0f;
-            }
-            float sq = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sq += v[i] * v[i];
-            const float inv = 1.0f / sqrtf(head_sum<L>(sq) * (1.0f / D) + A.eps);
-            if (!BACK) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = v[i] * inv * (isk ? gain[1][i] : gain[0][i]);
+        for (int w = 0; w < 2; ++w) {
+            float gain[16];
+            norm_load<ElemF32, PAIRED>(A.gain[w], l, A.rot, gain);
+            const int heads = A.heads[w], items = rows * heads * L;
+            const unsigned per = A.per_head[w];
+            // (the tile's first row is a scalar, 256 rows of a stride fit in 32 bits)
+            const E *x = (const E *)A.x[w] + r0 * A.xs[w], *dy = BACK ? (const E *)A.dy[w] + r0 * A.ds[w] : nullptr;
+            E *y = (E *)A.y[w] + r0 * A.ys[w];
+            const int xs = (int)A.xs[w], ds = (int)A.ds[w], ys = (int)A.ys[w];
+            for (int it = tid; it < items; it += kNormBlock) {
+                const int rh = it / L, r = over(rh, heads, per), h = rh - r * heads;
+                if (!live[r]) continue;  // the lanes of a head agree
+                float v[16], c[8], s[8];
+                norm_load<T, PAIRED>(x + (unsigned)(r * xs + h * D), l, A.rot, v);
                 if (turned) {
+                    const o_f32x4 *p = (const o_f32x4 *)&cs[2 * pairs * r + 8 * l], *q = (const o_f32x4 *)&cs[2 * pairs * r + pairs + 8 * l];
+                    const o_f32x4 c0 = p[0], c1 = p[1], s0 = q[0], s1 = q[1];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float a = v[i], b = v[8 + i];
-                        v[i] = a * c[i] - b * s[i];
-                        v[8 + i] = a * s[i] + b * c[i];
+                    for (int i = 0; i < 4; ++i) c[i] = c0[i], c[4 + i] = c1[i], s[i] = s0[i], s[4 + i] = s1[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) c[i] = 1.0f, s[i] = 0.0f;
+                }
+                float sq = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sq += v[i] * v[i];
+                const float inv = 1.0f / sqrtf(head_sum<L>(sq) * (1.0f / D) + A.eps);
+                if (!BACK) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = v[i] * inv * gain[i];
+                    if (turned) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float a = v[i], b = v[8 + i];
+                            v[i] = a * c[i] - b * s[i];
+                            v[8 + i] = a * s[i] + b * c[i];
+                        }
                     }
-                }
-            } else {
-                float d[16], dot = 0.0f;
-                norm_load<T, PAIRED>((const E *)A.dy[w] + (r0 + r) * A.ds[w] + (long long)hh * D, l, A.rot, d);
-                if (turned) {
+                } else {
+                    float d[16], dot = 0.0f;
+                    norm_load<T, PAIRED>(dy + (unsigned)(r * ds + h * D), l, A.rot, d);
+                    if (turned) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float a = d[i], b = d[8 + i];
-                        d[i] = a * c[i] + b * s[i];
-                        d[8 + i] = b * c[i] - a * s[i];
+                        for (int i = 0; i < 8; ++i) {
+                            const float a = d[i], b = d[8 + i];
+                            d[i] = a * c[i] + b * s[i];
+                            d[8 + i] = b * c[i] - a * s[i];
+                        }
                     }
-                }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    v[i] *= inv;
-                    const float g = d[i] * v[i];
-                    acc[0][i] += isk ? 0.0f : g;
-                    acc[1][i] += isk ? g : 0.0f;
-                    d[i] *= isk ? gain[1][i] : gain[0][i];
-                    dot += d[i] * v[i];
-                }
-                dot = head_sum<L>(dot) * (1.0f / D);
+                    for (int i = 0; i < 16; ++i) {
+                        v[i] *= inv;
+                        acc[w][i] += d[i] * v[i];
+                        d[i] *= gain[i];
+                        dot += d[i] * v[i];
+                    }
+                    dot = head_sum<L>(dot) * (1.0f / D);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = inv * (d[i] - v[i] * dot);
+                    for (int i = 0; i < 16; ++i) v[i] = inv * (d[i] - v[i] * dot);
+                }
+                norm_store<T, PAIRED>(y + (unsigned)(r * ys + h * D), l, A.rot, v);
             }
-            norm_store<T, PAIRED>((E *)A.y[w] + (r0 + r) * A.ys[w] + (long long)hh * D, l, A.rot, v);
         }
     }
     if (BACK) {
@@ -218,31 +237,37 @@ __global__ __launch_bounds__(kNormBlock) void tf_qk_norm_kernel(NormArgs A, Turn
     }
 }
 
-// dgain from the workgroups' partial sums, in their order: one workgroup per gain value.
+// dgain from the workgroups' partial sums, always in the same order: a workgroup has 64 of their 2 D columns, its 16
+// waves every 16th row.
 template <int D, bool PAIRED>
-__global__ __launch_bounds__(64) void tf_qk_norm_gain_kernel(const float *__restrict__ parts, int n, int rot,
-                                                              float *__restrict__ dq_gain, float *__restrict__ dk_gain) {
-    const int i = blockIdx.x % D, w = blockIdx.x / D, lane = threadIdx.x;
+__global__ __launch_bounds__(1024) void tf_qk_norm_gain_kernel(const float *__restrict__ parts, int n, int rot,
+                                                                float *__restrict__ dq_gain, float *__restrict__ dk_gain) {
+    __shared__ float sums[16][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = blockIdx.x * 64 + lane;
     float a = 0.0f;
-    for (int p = lane; p < n; p += 64) a += parts[(long long)p * 2 * D + w * D + i];
-    a = head_sum<64>(a);
-    if (lane == 0) {
-        const int l = i / 16, j = i % 16;  // the lane's j-th value: where norm_load took it from
+#pragma unroll 16
+    for (int p = wave; p < n; p += 16) a += parts[(long long)p * 2 * D + col];
+    sums[wave][lane] = a;
+    __syncthreads();
+    if (wave == 0) {
+        a = 0.0f;
+        for (int w = 0; w < 16; ++w) a += sums[w][lane];
+        const int i = col % D, l = i / 16, j = i % 16;  // lane l's j-th value: where norm_load took it from
         int at;
         if (PAIRED) at = 16 * l + 2 * (j % 8) + j / 8;
         else if (16 * l < rot) at = 8 * l + j % 8 + (j / 8) * (rot / 2);
         else at = 16 * l + j;
-        (w ? dk_gain : dq_gain)[at] = a;
+        (col / D ? dk_gain : dq_gain)[at] = a;
     }
 }
 
-// Rows of a tile: as many angles as the LDS array holds, fewer where that leaves compute units
-// without a tile.
+// Rows of a tile: as many angles as the LDS array holds, fewer where that leaves compute units without a tile; and so
+// that the tiles come out even for 1024 workgroups (the backward pass has no more; 1059 tiles took it twice 1024's time).
 int norm_tile(const tf_qk_norm_config *c, int64_t n_rows) {
-    const int most = kNormAngles / (c->rotary_dim / 2);
-    int64_t t = n_rows / 1024;
-    if (t < 1) t = 1;
-    return (int)(t < most ? t : most);
+    const int64_t most = kNormAngles / (c->rotary_dim / 2);
+    const int64_t rounds = (n_rows + 1024 * most - 1) / (1024 * most);
+    const int64_t t = rounds ? (n_rows + 1024 * rounds - 1) / (1024 * rounds) : 1;
+    return (int)(t < 1 ? 1 : t < most ? t : most);
 }
 
 tf_status norm_check(const tf_qk_norm_config *c, int64_t n_rows, int32_t n_seqs) {
@@ -253,7 +278,7 @@ tf_status norm_check(const tf_qk_norm_config *c, int64_t n_rows, int32_t n_seqs)
     if (!(c->eps >= 0.0f) || !(c->base > 0.0) || !std::isfinite(c->base) || !std::isfinite(c->eps)) return TF_EINVAL;
     const int d = c->head_dim;
     if ((d != 32 && d != 64 && d != 128 && d != 256) || c->rotary_dim % 16) return TF_EUNSUPPORTED;
-    if (c->n_q_heads > 4096 || c->n_k_heads > 4096 || n_rows > INT32_MAX) return TF_EUNSUPPORTED;
+    if (c->n_q_heads > 1024 || c->n_k_heads > 1024 || n_rows > INT32_MAX) return TF_EUNSUPPORTED;
     return TF_OK;
 }
 
@@ -287,9 +312,20 @@ template <bool BACK> void norm_width(const tf_qk_norm_config *c, const NormArgs 
 }
 template <int D> void gain_launch(const tf_qk_norm_config *c, const float *parts, int n, float *dq, float *dk, hipStream_t s) {
     if (c->interleaved)
-        hipLaunchKernelGGL((tf_qk_norm_gain_kernel<D, true>), dim3(2 * D), dim3(64), 0, s, parts, n, (int)c->rotary_dim, dq, dk);
+        hipLaunchKernelGGL((tf_qk_norm_gain_kernel<D, true>), dim3(2 * D / 64), dim3(1024), 0, s, parts, n, (int)c->rotary_dim, dq, dk);
     else
-        hipLaunchKernelGGL((tf_qk_norm_gain_kernel<D, false>), dim3(2 * D), dim3(64), 0, s, parts, n, (int)c->rotary_dim, dq, dk);
+        hipLaunchKernelGGL((tf_qk_norm_gain_kernel<D, false>), dim3(2 * D / 64), dim3(1024), 0, s, parts, n, (int)c->rotary_dim, dq, dk);
+}
+
+void norm_sizes(const tf_qk_norm_config *c, int64_t n_rows, NormArgs &A) {
+    auto per = [](unsigned n) { return n == 1 ? 0xffffffffu : (unsigned)((1ull << 32) / n); };
+    A.rot = c->rotary_dim, A.tile = norm_tile(c, n_rows), A.eps = c->eps;
+    A.per_head[0] = per((unsigned)c->n_q_heads), A.per_head[1] = per((unsigned)c->n_k_heads), A.per_pair = per((unsigned)c->rotary_dim / 2);
+}
+bool strides_fit(std::initializer_list<int64_t> strides) {
+    for (int64_t s : strides)
+        if (s > (1 << 22)) return false;
+    return true;
 }
 
 int64_t norm_blocks(const tf_qk_norm_config *c, int64_t n_rows, int64_t most) {
@@ -316,6 +352,7 @@ extern "C" tf_status tf_qk_norm_rotate(const tf_qk_norm_config *c, const void *q
     if (!stride_ok(q_stride, qw, c->elem) || !stride_ok(k_stride, kw, c->elem) || !stride_ok(q_out_stride, qw, c->elem) ||
         !stride_ok(k_out_stride, kw, c->elem))
         return TF_EINVAL;
+    if (!strides_fit({q_stride, k_stride, q_out_stride, k_out_stride})) return TF_EUNSUPPORTED;
     if (n_rows == 0) return TF_OK;
     if (!q || !k || !q_gain || !k_gain || !q_out || !k_out) return TF_EINVAL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(q_gain) || !aligned16(k_gain) || !aligned16(q_out) || !aligned16(k_out))
@@ -325,7 +362,7 @@ extern "C" tf_status tf_qk_norm_rotate(const tf_qk_norm_config *c, const void *q
     A.xs[0] = q_stride, A.xs[1] = k_stride, A.ys[0] = q_out_stride, A.ys[1] = k_out_stride;
     A.heads[0] = c->n_q_heads, A.heads[1] = c->n_k_heads;
     A.n_rows = n_rows, A.positions = positions, A.offsets = offsets, A.n_seqs = n_seqs;
-    A.rot = c->rotary_dim, A.tile = norm_tile(c, n_rows), A.eps = c->eps;
+    norm_sizes(c, n_rows, A);
     norm_width<false>(c, A, (int)norm_blocks(c, n_rows, 1 << 20), stream);
     return hipGetLastError() == hipSuccess ? TF_OK : TF_EHIP;
 }
@@ -343,6 +380,7 @@ extern "C" tf_status tf_qk_norm_rotate_backward(const tf_qk_norm_config *c, cons
     if (!stride_ok(q_stride, qw, c->elem) || !stride_ok(k_stride, kw, c->elem) || !stride_ok(dq_stride, qw, c->elem) ||
         !stride_ok(dk_stride, kw, c->elem) || !stride_ok(dq_out_stride, qw, c->elem) || !stride_ok(dk_out_stride, kw, c->elem))
         return TF_EINVAL;
+    if (!strides_fit({q_stride, k_stride, dq_stride, dk_stride, dq_out_stride, dk_out_stride})) return TF_EUNSUPPORTED;
     if (!q_gain || !k_gain || !dq_gain || !dk_gain || !workspace || !aligned16(q_gain) || !aligned16(k_gain)) return TF_EINVAL;
     if (workspace_bytes < tf_qk_norm_workspace_size(c, n_rows) || ((uintptr_t)workspace & 3)) return TF_EINVAL;
     if (n_rows > 0) {
@@ -357,7 +395,8 @@ extern "C" tf_status tf_qk_norm_rotate_backward(const tf_qk_norm_config *c, cons
     A.ys[0] = dq_stride, A.ys[1] = dk_stride;
     A.heads[0] = c->n_q_heads, A.heads[1] = c->n_k_heads;
     A.n_rows = n_rows, A.positions = positions, A.offsets = offsets, A.n_seqs = n_seqs;
-    A.rot = c->rotary_dim, A.tile = norm_tile(c, n_rows), A.eps = c->eps, A.parts = (float *)workspace;
+    norm_sizes(c, n_rows, A);
+    A.parts = (float *)workspace;
     int blocks = (int)norm_blocks(c, n_rows, kNormParts);
     if (blocks < 1) blocks = 1;  // no rows: the gradients of the gains are zeros
     norm_width<true>(c, A, blocks, stream);

@@ -69,14 +69,21 @@ def declare(L) -> None:
         f.restype, f.argtypes = res, args
 
 
+_loaded = None
+
+
 def _lib():
-    from . import lib
-    return lib()
+    global _loaded
+    if _loaded is None:
+        from . import lib
+        _loaded = lib()
+    return _loaded
 
 
 def _check(status: int, what: str):
-    from . import _check as check
-    check(status, what)
+    if status:
+        from . import TrackfitError
+        raise TrackfitError(status, what)
 
 
 @functools.lru_cache(maxsize=256)
