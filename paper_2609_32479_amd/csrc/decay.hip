@@ -142,22 +142,6 @@ __device__ __forceinline__ bool any_bad(const int *__restrict__ bad) {
     return b;
 }
 
-// Steps in order, step(i, fragment i), with the fragments of the next DEPTH - 1 steps on their way.  The fences keep that
-// order: left to itself the compiler reads a fragment, waits for it and only then multiplies, an LDS latency a step.
-template <int N, int DEPTH, class Load, class Step> __device__ __forceinline__ void in_turn(Load load, Step step) {
-    decltype(load(0)) w[DEPTH];
-#pragma unroll
-    for (int i = 0; i < DEPTH - 1; ++i)
-        if (i < N) w[i] = load(i);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        if (i + DEPTH - 1 < N) w[(i + DEPTH - 1) % DEPTH] = load(i + DEPTH - 1);
-        __builtin_amdgcn_sched_barrier(0);
-        step(i, w[i % DEPTH]);
-        __builtin_amdgcn_sched_barrier(0);
-    }
-}
-
 // Where the spans' borders are.
 struct Spans {
     const int2 *info;  // first and past-the-last row of each row's sequence, (-1, -1) outside of all

@@ -69,14 +69,24 @@ __device__ __forceinline__ void dma16(const void *src, unsigned lds) {
                  : "v"(src), "{m0}"(__builtin_amdgcn_readfirstlane(lds))
                  : "memory");
 }
-// All of the wave's loads into LDS have arrived and its reads are done; then the workgroup's.
-__device__ __forceinline__ void stage_barrier() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+// All but the wave's last LEFT loads into LDS have arrived and its reads are done; then the workgroup's.
+template <int LEFT> __device__ __forceinline__ void stage_barrier() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
 
-// act and act'.  The 16-bit types round the result to 2^-9 or 2^-12: the hardware's exp2 and reciprocal (2^-22) do.
+// act and act'.  The 16-bit types round the result to 2^-9 or 2^-12: the hardware's exp2 and reciprocal (2^-22) do, and for
+// Phi the approximation 7.1.26 of Abramowitz and Stegun (1.5e-7 off at most), which shares its exponential with the
+// derivative (with the library's erf the backward product's projections of 5003 x 1032 -> 2731 took 124 us, 47 with this).
 template <class T, bool GELU> __device__ __forceinline__ void act_of(float a, float &v, float &d) {
-    if constexpr (GELU) {
+    if constexpr (GELU && sizeof(typename T::E) == 2) {
+        const float x = fabsf(a) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * x);
+        const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * x * x);  // exp(-a^2 / 2)
+        const float y = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+        const float half = 0.5f * y * e;  // Phi(-|a|)
+        const float p = a < 0.0f ? half : 1.0f - half;
+        v = a * p;
+        d = p + a * (0.3989422804014327f * e);
+    } else if constexpr (GELU) {
         const float p = 0.5f * (1.0f + erff(a * 0.70710678118654752f));
         v = a * p;
         d = p + a * (0.3989422804014327f * expf(-0.5f * a * a));
@@ -115,7 +125,7 @@ enum { GATED_H = 0, GATED_D = 1, GATED_DX = 2, GATED_DW = 3 };
 //   H, D:  m = x along, n = W_g and W_u along (interleaved by wave)
 //   DX:    m = [da db] along, n = W_g, then W_u, across
 //   DW:    m = [da db] across, n = x across
-template <class T, int ROLE, int BM, int BN, int WM, int WN, bool GELU, bool SPLIT>
+template <class T, int ROLE, int BM, int BN, int WM, int WN, int STAGES, bool GELU, bool SPLIT>
 __global__ __launch_bounds__(64 * WM * WN) void tf_gated_kernel(GatedArgs A) {
     typedef typename T::E E;
     typedef typename Mma<T>::F F;
@@ -250,23 +260,26 @@ __global__ __launch_bounds__(64 * WM * WN) void tf_gated_kernel(GatedArgs A) {
     for (int i = 0; i < WTN; ++i)
 #pragma unroll
         for (int j = 0; j < WTM; ++j) acc[i][j] = o_f32x4{0.f, 0.f, 0.f, 0.f};
-    if (steps > 0) bring(0, 0);
+    // A ring of stages: step s's loads go out STAGES - 1 steps before it, into the slot that step s - STAGES has left.
+    for (int s = 0; s < STAGES - 1; ++s)
+        if (s < steps) bring(s, s);
+    int slot = 0, next = STAGES - 1;
     for (int s = 0; s < steps; ++s) {
-        stage_barrier();
-        if (s + 1 < steps) bring(s + 1, (s + 1) & 1);
-        const char *tm_ = smem + (s & 1) * STAGE, *tn_ = tm_ + BM * 128;
+        if (s + STAGES - 2 < steps) stage_barrier<(STAGES - 2) * (LM + LN)>();
+        else stage_barrier<0>();
+        if (s + STAGES - 1 < steps) bring(s + STAGES - 1, next);
+        const char *tm_ = smem + slot * STAGE, *tn_ = tm_ + BM * 128;
+        slot = slot + 1 < STAGES ? slot + 1 : 0;
+        next = next + 1 < STAGES ? next + 1 : 0;
+        F fn[SUBS][WTN];
 #pragma unroll
-        for (int sub = 0; sub < SUBS; ++sub) {
-            F fn[WTN];
+        for (int i = 0; i < SUBS * WTN; ++i) fn[i / WTN][i % WTN] = frag(tn_, NA, BN, wn * WTN + i % WTN, i / WTN);
+        in_turn<SUBS * WTM, 4>([&](int i) { return frag(tm_, MA, BM, wm * WTM + i % WTM, i / WTM); },
+                               [&](int i, F fm) {
 #pragma unroll
-            for (int i = 0; i < WTN; ++i) fn[i] = frag(tn_, NA, BN, wn * WTN + i, sub);
-#pragma unroll
-            for (int j = 0; j < WTM; ++j) {
-                const F fm = frag(tm_, MA, BM, wm * WTM + j, sub);
-#pragma unroll
-                for (int i = 0; i < WTN; ++i) acc[i][j] = Mma<T>::mma(fn[i], fm, acc[i][j]);
-            }
-        }
+                                   for (int e = 0; e < WTN; ++e)
+                                       acc[e][i % WTM] = Mma<T>::mma(fn[i / WTM][e], fm, acc[e][i % WTM]);
+                               });
     }
 
     typedef __attribute__((ext_vector_type(4))) E E4;
@@ -281,10 +294,30 @@ __global__ __launch_bounds__(64 * WM * WN) void tf_gated_kernel(GatedArgs A) {
         constexpr int HT = WTN / 2;
         const bool vec = ROLE == GATED_D || (A.os % 4 == 0 && ((size_t)A.out & (4 * ES - 1)) == 0);
         const bool dvec = ROLE == GATED_D && A.ds % 4 == 0 && ((size_t)A.dh & (4 * ES - 1)) == 0;
+        struct Row {
+            E4 g[HT];
+        };
+        // dh's rows are read two tiles ahead of their use
+        auto read = [&](int j) {
+            Row r = {};
+            if constexpr (ROLE == GATED_D) {
+                long long m = m0 + 16 * (wm * WTM + j) + n;
+                if (m >= A.M) m = A.M - 1;
 #pragma unroll
-        for (int j = 0; j < WTM; ++j) {
+                for (int i = 0; i < HT; ++i) {
+                    const int f = tn * (BN / 2) + 16 * (wn * HT + i) + 4 * q;
+                    const E *p = (const E *)A.dh + m * A.ds;
+                    if (dvec && f + 4 <= A.F) r.g[i] = *(const E4 *)(p + f);
+                    else
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) r.g[i][e] = p[f + e < A.F ? f + e : A.F - 1];
+                }
+            }
+            return r;
+        };
+        in_turn<WTM, 3>(read, [&](int j, const Row &row) {
             const long long m = m0 + 16 * (wm * WTM + j) + n;
-            if (m >= A.M) continue;
+            if (m >= A.M) return;
 #pragma unroll
             for (int i = 0; i < HT; ++i) {
                 const int f = tn * (BN / 2) + 16 * (wn * HT + i) + 4 * q, left = A.F - f;
@@ -300,12 +333,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tf_gated_kernel(GatedArgs A) {
                     if (left > 0) put((E *)A.out + m * A.os + f, vec, left, v * b);
                 } else {
                     if (f >= A.Fp) continue;
-                    o_f32x4 g = {0.f, 0.f, 0.f, 0.f};
-                    const E *p = (const E *)A.dh + m * A.ds + f;
-                    if (dvec && left >= 4) g = __builtin_convertvector(*(const E4 *)p, o_f32x4);
-                    else
-                        for (int e = 0; e < 4; ++e)
-                            if (e < left) g[e] = (float)p[e];
+                    const o_f32x4 g = __builtin_convertvector(row.g[i], o_f32x4);
                     o_f32x4 da = g * b * d, db = g * v;
 #pragma unroll
                     for (int e = 0; e < 4; ++e)  // the padding is zeros whatever the sums of the clamped rows are
@@ -315,7 +343,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tf_gated_kernel(GatedArgs A) {
                     put(o + A.Fp, true, 4, db);
                 }
             }
-        }
+        });
     } else {
         const bool vec = A.os % 4 == 0 && ((size_t)A.out & (4 * ES - 1)) == 0 && (ROLE == GATED_DX || ((size_t)A.out2 & (4 * ES - 1)) == 0);
 #pragma unroll
@@ -433,17 +461,34 @@ tf_status gated_check(const tf_gated_config *c, int64_t n_rows) {
 }
 int64_t gated_pad(const tf_gated_config *c) { return ((int64_t)c->inner + 63) / 64 * 64; }
 
-// Parts of a sum of length k over `tiles` tiles of 128 x 128: as many as give every compute unit a workgroup or two,
+// The tiles of a product of m x n, the first a wave's two-deep ring of 64 KB stages, the others of three and four: what
+// bounds a tile is its products (a quarter of them each time the tile's sides shrink to half, at 0.9 and 0.75 of the rate,
+// as the fragments' reads grow against them), and whole rounds of 256 compute units are paid for.
+struct Shape {
+    int m, n;
+};
+constexpr Shape kShapes[3] = {{256, 256}, {256, 128}, {128, 128}};
+constexpr double kShapeRate[3] = {1.0, 0.9, 0.75};
+int64_t gated_tiles(int64_t m, int64_t n, int shape) {
+    return ((m + kShapes[shape].m - 1) / kShapes[shape].m) * ((n + kShapes[shape].n - 1) / kShapes[shape].n);
+}
+int gated_shape(int64_t m, int64_t n) {
+    int best = 0;
+    double least = 0.0;
+    for (int i = 0; i < 3; ++i) {
+        const double t = (double)((gated_tiles(m, n, i) + 255) / 256) * kShapes[i].m * kShapes[i].n / kShapeRate[i];
+        if (i == 0 || t < least) best = i, least = t;
+    }
+    return best;
+}
+// Parts of a sum of length k over `tiles` tiles of 128 x 128: as many as give every compute unit a workgroup,
 // each at least 512 long (its products then take longer than its fp32 part's way out and back).
 int gated_parts(int64_t tiles, int64_t k) {
-    int64_t p = 512 / (tiles < 1 ? 1 : tiles);
+    int64_t p = 256 / (tiles < 1 ? 1 : tiles);
     if (p > k / 512) p = k / 512;
     if (p > 32) p = 32;
     return p < 1 ? 1 : (int)p;
 }
-int64_t gated_tiles(int64_t m, int64_t n, int b) { return ((m + b - 1) / b) * ((n + b - 1) / b); }
-// 256 x 256 tiles move half the LDS bytes a flop of 128 x 128 ones, and are taken where they fill the compute units.
-bool gated_big(int64_t m, int64_t n) { return gated_tiles(m, n, 256) >= 192; }
 
 struct GatedPlan {
     int64_t fp, dx_parts, dw_parts;
@@ -452,8 +497,8 @@ struct GatedPlan {
 GatedPlan gated_plan(const tf_gated_config *c, int64_t m) {
     GatedPlan p = {};
     p.fp = gated_pad(c);
-    p.dx_parts = gated_big(m, c->width) ? 1 : gated_parts(gated_tiles(m, c->width, 128), 2 * p.fp);
-    p.dw_parts = gated_big(2 * p.fp, c->width) ? 1 : gated_parts(gated_tiles(2 * p.fp, c->width, 128), m);
+    p.dx_parts = gated_parts(gated_tiles(m, c->width, 2), 2 * p.fp);
+    p.dw_parts = gated_parts(gated_tiles(2 * p.fp, c->width, 2), m);
     p.dgu = ((size_t)m * 2 * p.fp * elem_bytes(c->elem) + 255) / 256 * 256;
     const size_t a = p.dx_parts > 1 ? (size_t)p.dx_parts * m * c->width * 4 : 0;
     const size_t b = p.dw_parts > 1 ? (size_t)p.dw_parts * 2 * p.fp * c->width * 4 : 0;
@@ -462,28 +507,30 @@ GatedPlan gated_plan(const tf_gated_config *c, int64_t m) {
     return p;
 }
 
-template <class T, int ROLE, int B, bool GELU, bool SPLIT> tf_status gated_tile(GatedArgs A, int parts, hipStream_t s) {
-    constexpr int WM = 2, WN = B == 256 ? 4 : 2;
-    constexpr int LDS = 2 * (B + B) * 128;
-    constexpr int BNC = ROLE == GATED_H || ROLE == GATED_D ? B / 2 : B;  // inner values of a tile
-    A.tiles_m = (int)((A.M + B - 1) / B);
-    A.tiles_n = (int)((A.N + BNC - 1) / BNC);
-    auto kernel = tf_gated_kernel<T, ROLE, B, B, WM, WN, GELU, SPLIT>;
+template <class T, int ROLE, int SHAPE, bool GELU, bool SPLIT> void gated_tile(GatedArgs A, int parts, hipStream_t s) {
+    constexpr int BM = kShapes[SHAPE].m, BN = kShapes[SHAPE].n, WM = SHAPE == 1 ? 4 : 2, WN = SHAPE == 0 ? 4 : 2;
+    constexpr int STAGES = SHAPE + 2, LDS = STAGES * (BM + BN) * 128;
+    constexpr int inner = ROLE == GATED_H || ROLE == GATED_D ? BN / 2 : BN;  // inner values of a tile
+    A.tiles_m = (int)((A.M + BM - 1) / BM);
+    A.tiles_n = (int)((A.N + inner - 1) / inner);
+    auto kernel = tf_gated_kernel<T, ROLE, BM, BN, WM, WN, STAGES, GELU, SPLIT>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)A.tiles_m * A.tiles_n), SPLIT ? parts : 1), dim3(64 * WM * WN), LDS, s, A);
-    return TF_OK;
 }
-template <class T, int ROLE, bool GELU> void gated_product(const GatedArgs &A, bool big, int parts, hipStream_t s) {
+template <class T, int ROLE, bool GELU> void gated_product(const GatedArgs &A, int parts, hipStream_t s) {
     if constexpr (ROLE == GATED_DX || ROLE == GATED_DW) {
         if (parts > 1) {
-            gated_tile<T, ROLE, 128, GELU, true>(A, parts, s);
+            gated_tile<T, ROLE, 2, GELU, true>(A, parts, s);
             const int64_t blocks = (A.M * A.N / 4 + 255) / 256;
             hipLaunchKernelGGL((tf_gated_join_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, s, A.part, parts, A.M, A.N, A.F, A.Fp,
                                ROLE == GATED_DW, A.out, A.out2, A.os);
             return;
         }
     }
-    if (big) gated_tile<T, ROLE, 256, GELU, false>(A, 1, s);
-    else gated_tile<T, ROLE, 128, GELU, false>(A, 1, s);
+    switch (gated_shape(A.M, ROLE == GATED_H || ROLE == GATED_D ? 2 * A.N : A.N)) {
+        case 0: gated_tile<T, ROLE, 0, GELU, false>(A, 1, s); break;
+        case 1: gated_tile<T, ROLE, 1, GELU, false>(A, 1, s); break;
+        default: gated_tile<T, ROLE, 2, GELU, false>(A, 1, s); break;
+    }
 }
 template <class T, bool BACK, bool GELU> void gated_project(const GatedArgs &A, hipStream_t s) {
     if (A.M <= kFewRows) {
@@ -493,7 +540,7 @@ template <class T, bool BACK, bool GELU> void gated_project(const GatedArgs &A, 
         else hipLaunchKernelGGL((tf_gated_rows_kernel<T, 4, BACK, GELU>), grid, block, 0, s, A);
         return;
     }
-    gated_product<T, BACK ? GATED_D : GATED_H, GELU>(A, gated_big(A.M, 2 * A.N), 1, s);
+    gated_product<T, BACK ? GATED_D : GATED_H, GELU>(A, 1, s);
 }
 template <class T> void gated_forward(const tf_gated_config *c, const GatedArgs &A, hipStream_t s) {
     if (c->activation == TF_ACT_GELU) gated_project<T, false, true>(A, s);
@@ -502,8 +549,8 @@ template <class T> void gated_forward(const tf_gated_config *c, const GatedArgs 
 template <class T> void gated_backward(const tf_gated_config *c, const GatedArgs &P, const GatedArgs &X, const GatedArgs &W, const GatedPlan &p, hipStream_t s) {
     if (c->activation == TF_ACT_GELU) gated_project<T, true, true>(P, s);
     else gated_project<T, true, false>(P, s);
-    gated_product<T, GATED_DX, false>(X, gated_big(X.M, X.N), (int)p.dx_parts, s);
-    gated_product<T, GATED_DW, false>(W, gated_big(W.M, W.N), (int)p.dw_parts, s);
+    gated_product<T, GATED_DX, false>(X, (int)p.dx_parts, s);
+    gated_product<T, GATED_DW, false>(W, (int)p.dw_parts, s);
 }
 
 }  // namespace
@@ -567,9 +614,9 @@ extern "C" tf_status tf_gated_ffn_backward(const tf_gated_config *c, const void 
     W.k_per = (int)(((n_rows + 63) / 64 + p.dw_parts - 1) / p.dw_parts * 64);
     if (n_rows == 0) {
         // no tokens: the weights' gradients are zeros (a product over an empty sum)
-        if (c->elem == TF_ELEM_BF16) gated_product<ElemBF16, GATED_DW, false>(W, false, 1, stream);
-        else if (c->elem == TF_ELEM_FP32) gated_product<ElemF32, GATED_DW, false>(W, false, 1, stream);
-        else gated_product<ElemF16, GATED_DW, false>(W, false, 1, stream);
+        if (c->elem == TF_ELEM_BF16) gated_product<ElemBF16, GATED_DW, false>(W, 1, stream);
+        else if (c->elem == TF_ELEM_FP32) gated_product<ElemF32, GATED_DW, false>(W, 1, stream);
+        else gated_product<ElemF16, GATED_DW, false>(W, 1, stream);
     } else if (c->elem == TF_ELEM_BF16) gated_backward<ElemBF16>(c, P, X, W, p, stream);
     else if (c->elem == TF_ELEM_FP32) gated_backward<ElemF32>(c, P, X, W, p, stream);
     else gated_backward<ElemF16>(c, P, X, W, p, stream);

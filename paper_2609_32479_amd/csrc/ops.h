@@ -54,6 +54,22 @@ __device__ __forceinline__ int seq_of_row(const int32_t *__restrict__ offsets, i
     return lo - 1;
 }
 
+// Steps in order, step(i, fragment i), with the fragments of the next DEPTH - 1 steps on their way.  The fences keep that
+// order: left to itself the compiler reads a fragment, waits for it and only then multiplies, an LDS latency a step.
+template <int N, int DEPTH, class Load, class Step> __device__ __forceinline__ void in_turn(Load load, Step step) {
+    decltype(load(0)) w[DEPTH];
+#pragma unroll
+    for (int i = 0; i < DEPTH - 1; ++i)
+        if (i < N) w[i] = load(i);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (i + DEPTH - 1 < N) w[(i + DEPTH - 1) % DEPTH] = load(i + DEPTH - 1);
+        __builtin_amdgcn_sched_barrier(0);
+        step(i, w[i % DEPTH]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 inline size_t elem_bytes(int e) { return e == TF_ELEM_FP32 ? 4 : 2; }
 inline bool elem_ok(int e) { return e == TF_ELEM_FP32 || e == TF_ELEM_BF16 || e == TF_ELEM_FP16; }
