@@ -263,6 +263,47 @@ template <class T> __device__ __forceinline__ void store4(typename T::E *p, o_f3
     *(V *)p = __builtin_convertvector(v, V);
 }
 
+// v of another lane of the same 16 (DPP; 0 where there is none).
+template <int CTRL> __device__ __forceinline__ float dpp(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+template <int CTRL> __device__ __forceinline__ double dpp(double v) {
+    const long long b = __builtin_bit_cast(long long, v);
+    const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)b, CTRL, 0xf, 0xf, false);
+    const unsigned hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, 0xf, 0xf, false);
+    return __builtin_bit_cast(double, (long long)((unsigned long long)hi << 32 | lo));
+}
+__device__ __forceinline__ double lane_of(double v, int lane) {
+    const long long b = __builtin_bit_cast(long long, v);
+    const unsigned lo = __builtin_amdgcn_readlane((int)b, lane), hi = __builtin_amdgcn_readlane((int)(b >> 32), lane);
+    return __builtin_bit_cast(double, (long long)((unsigned long long)hi << 32 | lo));
+}
+// The sum over the 16 lanes of a row, in all of them: neighbours, pairs, quads, halves.
+__device__ __forceinline__ float sum16(float v) {
+    v += dpp<0xb1>(v);   // quad_perm 1 0 3 2
+    v += dpp<0x4e>(v);   // quad_perm 2 3 0 1
+    v += dpp<0x141>(v);  // row_half_mirror
+    v += dpp<0x140>(v);  // row_mirror
+    return v;
+}
+// v summed over the lanes from `from` (this lane's own, at most this lane) to this one.
+__device__ __forceinline__ double sum_from(double v, int from, int lane) {
+    const int in = lane & 15;
+    auto step = [&](double o, int d) {
+        if (in >= d && lane - d >= from) v += o;
+    };
+    step(dpp<0x111>(v), 1);  // row_shr
+    step(dpp<0x112>(v), 2);
+    step(dpp<0x114>(v), 4);
+    step(dpp<0x118>(v), 8);
+#pragma unroll
+    for (int r = 16; r < 64; r += 16) {  // the rows of 16 before: their last lane's sum is of the same run
+        const double o = lane_of(v, r - 1);
+        if (lane >= r && lane < r + 16 && from < r) v += o;
+    }
+    return v;
+}
+
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 // 2^x of an fp64 x, to fp32's precision
 __device__ __forceinline__ float exp2_of(double x) {
@@ -283,10 +324,18 @@ __device__ __forceinline__ int seg_first(int s) { return (s & 255) - 1; }
 __device__ __forceinline__ int seg_past(int s) { return (s >> 8) & 255; }
 __device__ __forceinline__ bool seg_ends(int s) { return s >> 16; }
 
+// The tiles of a chunk's weights on or below the diagonal, two bits each, in the order in which they are dealt to four
+// waves: the last wave, which has the next chunk's rows to prepare, gets two of the far ones, which short sequences skip.
+constexpr int tile_list(int a, int b, int c, int d, int e, int f, int g, int h, int i, int j) {
+    return a | b << 2 | c << 4 | d << 6 | e << 8 | f << 10 | g << 12 | h << 14 | i << 16 | j << 18;
+}
+constexpr int kTileT = tile_list(3, 2, 1, 3, 0, 3, 2, 2, 1, 3), kTileS = tile_list(3, 2, 1, 0, 0, 2, 1, 0, 0, 1);
+__device__ __forceinline__ int tile_of(int list, int w) { return list >> (2 * w) & 3; }
+
 // One span of one head, four waves.  A wave owns a quarter of the state's and the output's columns (d_v 32: half, and
 // of the outputs every second row tile; its pair holds the same state); the state stays in its accumulators over the span.  The 64 x 64 weights of a chunk are computed once,
-// 16 x 16 tiles on or below the diagonal dealt out to the waves, and pass through LDS.  The next chunk's rows of
-// the tensors are on their way to registers meanwhile, and its row sums are one wave's work beside the products.
+// 16 x 16 tiles on or below the diagonal dealt out to the waves, and pass through LDS; the last
+// wave prepares the next chunk's row sums meanwhile.  The next chunk's rows of the tensors are on their way to registers.
 template <class T, int DK, int DV, int MODE>
 __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ? 4 : 3) : MODE == DECAY_OUT && DK * DV <= 64 * 64 ? 3 : 2) void tf_decay_span_kernel(DecayRuns R) {
     typedef typename MatOf<T>::M M;
@@ -424,19 +473,14 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         if (i >= rows) f = l = i;  // behind the last row: on its own
         const float g = next_g < kForget ? kForget : next_g;  // (NaN stays)
         double b = i >= rows || (A.shift && f == i) ? 0.0 : (double)g * 1.4426950408889634;
-        const int from = f > 0 ? f : 0;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const double o = __shfl_up(b, d);
-            if (i - d >= from) b += o;
-        }
+        b = sum_from(b, f > 0 ? f : 0, i);
         const int e = l < rows - 1 ? l : rows - 1;
         const double be = __shfl(b, e & 63);
         const float bf = (float)b, de = exp2_of(b);
         W.bh[i] = bf, W.bl[i] = (float)(b - (double)bf);
         W.decay[i] = de, W.in[i] = A.out_scale * de, W.to[i] = A.kv_scale * exp2_of(be - b);
         W.seg[i] = (f < 0 ? 0 : f + 1) | (i < rows ? e + 1 : i + 1) << 8 | (l <= rows - 1 ? 1 << 16 : 0);
-        if (!OUT) total += __shfl(b, rows - 1);
+        if (!OUT) total += lane_of(b, rows - 1);
     };
     // What a chunk's loads bring goes to LDS when the chunk before is done with it.  The registers in between are this
     // chunk's own (carried around the loop they would be copied at its end, and waited for there).
@@ -453,6 +497,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
     if (wave == NW - 1) {
         fetch_rows(0);
         put_rows(rows_of[0], 0);
+        fetch_rows(1);
     }
     if (OUT)  // the weights above the diagonal that share a fragment with some below
         for (int i = tid; i < kChunk * LP * (int)sizeof(ME) / 4; i += NT) ((unsigned *)Ps)[i] = 0;
@@ -465,14 +510,22 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         const ChunkRows &W = rows_of[c & 1];
         const bool slow = __builtin_amdgcn_readfirstlane(wild[c & 1]);
         fetch(c + 1);
-        if (wave == NW - 1) fetch_rows(c + 1);
-
+        F vf[NB][CT];  // the wave's columns of v, for the state and for the output
+#pragma unroll
+        for (int k = 0; k < NB; ++k)
+#pragma unroll
+            for (int j = 0; j < CT; ++j) vf[k][j] = M::down(Vs, LV, k * KM, c0 + 16 * j, n, q);
+        // the last wave prepares the next chunk's rows while the others compute the weights
+        if (wave == NW - 1 && c + 1 < chunks) {
+            put_rows(rows_of[(c + 1) & 1], c + 1);
+            fetch_rows(c + 2);
+        }
         if (OUT) {
             // weights: tile (s tile ms, t tile mt), transposed, so that four consecutive s of a row t land in a lane
             const float sc = A.out_scale * A.kv_scale;
 #pragma unroll 1
-            for (int w = wave; w < 10; w += NW) {
-                const int mt = w < 4 ? 3 : w < 7 ? 2 : w < 9 ? 1 : 0, ms = w < 4 ? w : w < 7 ? w - 4 : w < 9 ? w - 7 : 0;
+            for (int w = NW == 4 || wave < NW - 1 ? wave : 10; w < 10; w += NW == 4 ? NW : NW - 1) {
+                const int mt = tile_of(kTileT, w), ms = tile_of(kTileS, w);
                 const int t = 16 * mt + n, s = 16 * ms + 4 * q, f = seg_first(W.seg[t]);
                 const bool apart = seg_first(__builtin_amdgcn_readfirstlane(W.seg[16 * mt])) >= 16 * ms + 16;  // all of the tile's rows are of later sequences
                 typedef __attribute__((ext_vector_type(4))) ME V4;
@@ -509,9 +562,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                     row += __shfl_xor(row, 32);
                     if (q == 0) rowp[ms][t] = row;
 #pragma unroll
-                    for (int d = 1; d < 16; d *= 2)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) z[i] += __shfl_xor(z[i], d);
+                    for (int i = 0; i < 4; ++i) z[i] = sum16(z[i]);
                     if (n == 0) *(o_f32x4 *)&colp[mt][s] = z;
                 }
             }
@@ -591,7 +642,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                         for (int i = 0; i < KM / 4; i += 4) *(o_f32x4 *)&w[i] = *(const o_f32x4 *)&W.to[k * KM + KM / 4 * q + i];
 #pragma unroll
                         for (int j = 0; j < CT; ++j) {
-                            const F v = M::down(Vs, LV, k * KM, c0 + 16 * j, n, q);
+                            const F v = vf[k][j];
                             float x[KM / 4];
 #pragma unroll
                             for (int i = 0; i < KM / 4; ++i) {
@@ -651,7 +702,6 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                 }
             }
             if (!slow) {
-                F v[CT];
                 in_turn<NB * TM, 4>(
                     [&](int i) {
                         F f = {};
@@ -660,13 +710,9 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                     },
                     [&](int i, F f) {
                         const int k = i / TM, m = i % TM;
-                        if (m == 0) {
-#pragma unroll
-                            for (int j = 0; j < CT; ++j) v[j] = M::down(Vs, LV, k * KM, c0 + 16 * j, n, q);
-                        }
                         if (k * KM <= 16 * row_tile(m)) {
 #pragma unroll
-                            for (int j = 0; j < CT; ++j) o[j][m] = M::mma(v[j], f, o[j][m]);
+                            for (int j = 0; j < CT; ++j) o[j][m] = M::mma(vf[k][j], f, o[j][m]);
                         }
                     });
             } else {
@@ -698,7 +744,6 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                 }
             }
         }
-        if (wave == NW - 1 && c + 1 < chunks) put_rows(rows_of[(c + 1) & 1], c + 1);
         __syncthreads();
         if (tid == 0) wild[c & 1] = 0;
         put(c + 1);
@@ -787,21 +832,20 @@ __global__ __launch_bounds__(256) void tf_decay_index_kernel(const int32_t *__re
     }
 }
 
-// The states at the spans' ends from the spans' own contributions, in order along each cut sequence.  A wave has 256
-// values of one head's states and every kChains-th span; where that is a sequence's first cut it follows the sequence, the
+// The states at the spans' ends from the spans' own contributions, in order along each cut sequence.  A wave has 128
+// values of one head's states and every `chains`-th span; where that is a sequence's first cut it follows the sequence, the
 // next spans' contributions on their way while it adds (each sum stays for the span that follows).
-constexpr int kChains = 16;
-__global__ __launch_bounds__(256) void tf_decay_chain_kernel(DecayRuns R, int size) {
+__global__ __launch_bounds__(256) void tf_decay_chain_kernel(DecayRuns R, int size, int chains) {
     const DecayRun &A = R.run[blockIdx.z];
     if (any_bad(A.bad)) return;
     const int heads = A.heads, spans = A.spans.n, dir = A.dir, lane = threadIdx.x % 64;
-    const int h = blockIdx.x / (kChains / 4), e = (blockIdx.y * 64 + lane) * 4;
+    const int h = blockIdx.x / (chains / 4), e = (blockIdx.y * 64 + lane) * 2;
     const long long step = (long long)dir * heads * size;
-    for (int first = blockIdx.x % (kChains / 4) * 4 + threadIdx.x / 64; first < spans; first += kChains * 64) {
-        const int mine = first + kChains * lane;
+    for (int first = blockIdx.x % (chains / 4) * 4 + threadIdx.x / 64; first < spans; first += chains * 64) {
+        const int mine = first + chains * lane;
         unsigned long long starts = __ballot(mine < spans && A.kind[mine < spans ? mine : 0] == 1);
         while (starts) {
-            const int p = first + kChains * __builtin_ctzll(starts);
+            const int p = first + chains * __builtin_ctzll(starts);
             starts &= starts - 1;
             int cuts = 0;
             for (int i = p + dir; i >= 0 && i < spans; i += 64 * dir) {  // how many spans it goes on through whole
@@ -815,17 +859,17 @@ __global__ __launch_bounds__(256) void tf_decay_chain_kernel(DecayRuns R, int si
             if (cuts == 0) continue;
             float *l = A.local + ((long long)p * heads + h) * size + e;
             const float *m = A.mult + (long long)p * heads + h;
-            o_f32x4 s = *(const o_f32x4 *)l;
+            o_f32x2 s = *(const o_f32x2 *)l;
             // Batches in turn, so that a batch's loads are waited for behind the next one's and not behind its stores (stores
             // under a branch would be waited for one by one: behind the end the last sum is stored again).
             constexpr int BATCH = 8;
-            o_f32x4 x[2][BATCH];
+            o_f32x2 x[2][BATCH];
             float w[2][BATCH];
             auto load = [&](int b, int i) {
 #pragma unroll
                 for (int j = 0; j < BATCH; ++j) {
                     const int k = i + j < cuts ? i + j + 1 : cuts;
-                    x[b][j] = *(const o_f32x4 *)(l + k * step), w[b][j] = m[(long long)k * dir * heads];
+                    x[b][j] = *(const o_f32x2 *)(l + k * step), w[b][j] = m[(long long)k * dir * heads];
                 }
             };
             auto add = [&](int b, int i) {
@@ -833,7 +877,7 @@ __global__ __launch_bounds__(256) void tf_decay_chain_kernel(DecayRuns R, int si
                 for (int j = 0; j < BATCH; ++j) {
                     const bool in = i + j < cuts;
                     if (in) s = x[b][j] + s * w[b][j];
-                    *(o_f32x4 *)(l + (in ? i + j + 1 : cuts) * step) = s;
+                    *(o_f32x2 *)(l + (in ? i + j + 1 : cuts) * step) = s;
                 }
             };
             load(0, 0);
@@ -942,14 +986,9 @@ __global__ __launch_bounds__(64) void tf_decay_grad_kernel(DecayGrad A) {
             v = (double)A.da[(long long)r * A.heads + h] - (double)A.db[(long long)r * A.heads + h];
             if (f == i && A.last) v += (double)A.last[(long long)seq_of_row(A.offsets, A.n_seqs, r) * A.heads + h];
         }
-        const int from = f > 0 ? f : 0;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const double o = __shfl_up(v, d);
-            if (i - d >= from) v += o;
-        }
+        v = sum_from(v, f > 0 ? f : 0, i);
         if (f < 0) v += carry;
-        carry = __shfl(v, 63);  // (the rows of a chunk before the last are 64)
+        carry = lane_of(v, 63);  // (the rows of a chunk before the last are 64)
         if (live) {
             const float g = A.gs ? A.g[(long long)r * A.gs + h] : A.g[h];
             if (g < -104.0f) v = 0.0;  // exp(g) is 0, and so is what it is multiplied with
@@ -1042,10 +1081,12 @@ tf_status decay_check(const tf_decay_config *c) {
     return TF_OK;
 }
 
-// Rows of a span.  Enough spans that four workgroups fit each compute unit, and no more than that: every
-// border that cuts a sequence costs a state written and read.
+// Rows of a span.  Enough spans that the compute units have four workgroups each (two of the wide heads', which hold
+// fewer), and no more than that: every border that cuts a sequence costs a state written and read.  32 768 rows of 8 heads of
+// 128 x 128, the three launches: spans of 128 366 us, 256 281, 512 234, 1024 303.  Not beyond 512 rows: the last workgroups'
+// share of 918 161 rows of tracks grows (spans of 512 407 us, 1024 413, 2048 437).
 int decay_span(const tf_decay_config *c, int64_t n_rows) {
-    int64_t s = n_rows * c->n_heads / 1024 / kChunk * kChunk;
+    int64_t s = n_rows * c->n_heads / (c->d_k * c->d_v > 64 * 64 ? 512 : 1024) / kChunk * kChunk;
     if (s < kMinSpan) s = kMinSpan;
     if (s > 512) s = 512;
     return (int)s;
@@ -1130,8 +1171,12 @@ void chain_run(int elem, DecayRuns R, int runs, int dk, int dv, hipStream_t s) {
     if (A.spans.n < 2) return;
     for (int i = 0; i < runs; ++i) R.run[i].sf = nullptr, R.run[i].turned = 0;
     span_run(elem, R, runs, dk, dv, DECAY_STATE, s);
-    hipLaunchKernelGGL(tf_decay_chain_kernel, dim3((unsigned)(kChains / 4 * A.heads), (unsigned)(dk * dv / 256), runs), dim3(256), 0, s, R,
-                       dk * dv);
+    // (as many waves for the chains as are on the chip at once: one without a chain still takes 4 us)
+    const int64_t pieces = (int64_t)A.heads * (dk * dv / 128) * runs;
+    int chains = (int)(1024 / pieces) * 4;
+    chains = chains < 4 ? 4 : chains > 64 ? 64 : chains;
+    hipLaunchKernelGGL(tf_decay_chain_kernel, dim3((unsigned)(chains / 4 * A.heads), (unsigned)(dk * dv / 128), runs), dim3(256), 0, s, R,
+                       dk * dv, chains);
 }
 void index_run(const int32_t *offsets, int n_seqs, int64_t n_rows, const Plan &p, int32_t *flags, hipStream_t s) {
     hipLaunchKernelGGL(tf_decay_index_kernel, dim3((unsigned)(kCheckers + (n_rows + kIndexRows - 1) / kIndexRows)), dim3(256), 0, s, offsets, n_seqs,

@@ -69,14 +69,19 @@ __device__ __forceinline__ void dma16(const void *src, unsigned lds) {
                  : "v"(src), "{m0}"(__builtin_amdgcn_readfirstlane(lds))
                  : "memory");
 }
-// All but the wave's last LEFT loads into LDS have arrived and its reads are done; then the workgroup's.
-template <int LEFT> __device__ __forceinline__ void stage_barrier() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+// The same from a scalar base and an offset for each lane.
+__device__ __forceinline__ void dma16(const char *base, unsigned off, unsigned lds) {
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                 :
+                 : "v"(off), "s"(base), "{m0}"(__builtin_amdgcn_readfirstlane(lds))
+                 : "memory");
 }
+// The wave's loads into LDS have arrived and its reads are done; then the workgroup's.
+__device__ __forceinline__ void stage_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // act and act'.  The 16-bit types round the result to 2^-9 or 2^-12: the hardware's exp2 and reciprocal (2^-22) do, and for
 // Phi the approximation 7.1.26 of Abramowitz and Stegun (1.5e-7 off at most), which shares its exponential with the
-// derivative (with the library's erf the backward product's projections of 5003 x 1032 -> 2731 took 124 us, 47 with this).
+// derivative.
 template <class T, bool GELU> __device__ __forceinline__ void act_of(float a, float &v, float &d) {
     if constexpr (GELU && sizeof(typename T::E) == 2) {
         const float x = fabsf(a) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * x);
@@ -125,8 +130,8 @@ enum { GATED_H = 0, GATED_D = 1, GATED_DX = 2, GATED_DW = 3 };
 //   H, D:  m = x along, n = W_g and W_u along (interleaved by wave)
 //   DX:    m = [da db] along, n = W_g, then W_u, across
 //   DW:    m = [da db] across, n = x across
-template <class T, int ROLE, int BM, int BN, int WM, int WN, int STAGES, bool GELU, bool SPLIT>
-__global__ __launch_bounds__(64 * WM * WN) void tf_gated_kernel(GatedArgs A) {
+template <class T, int ROLE, int BM, int BN, int WM, int WN, bool GELU, bool SPLIT>
+__global__ __launch_bounds__(64 * WM * WN, 2) void tf_gated_kernel(GatedArgs A) {
     typedef typename T::E E;
     typedef typename Mma<T>::F F;
     constexpr int NT = 64 * WM * WN, KS = Mma<T>::KS, SUBS = KS / Mma<T>::KM, ES = sizeof(E);
@@ -157,9 +162,10 @@ __global__ __launch_bounds__(64 * WM * WN) void tf_gated_kernel(GatedArgs A) {
     const int k_end = SPLIT ? (A.K - k_begin < A.k_per ? A.K : k_begin + A.k_per) : A.K;
     const int steps = (k_end - k_begin + KS - 1) / KS;
 
-    // Where each piece comes from.
-    const char *mp[LM], *np[LN];
-    int mk[LM], nk[LN];  // along: its first value of the sum; across: its row, within a step
+    // Where each piece comes from: a scalar that moves along the sum, and an offset of the lane's own (32 bits: at most 256
+    // rows of 2^20 values).  Rows and columns past the end are read as the last ones; what they give is not stored.
+    unsigned mo[LM], no[LN];
+    int mk[LM], nk[LN];  // the piece's first place along the sum within a step
     auto across_of = [&](int piece, int cols, int &row, int &col) {
         const int per = cols * ES / 16, slot = piece % per;
         row = piece / per;
@@ -171,71 +177,79 @@ __global__ __launch_bounds__(64 * WM * WN) void tf_gated_kernel(GatedArgs A) {
             col = ((((slot >> 2) ^ g) << 2) | (slot & 3)) * 4;
         }
     };
+    const long long n0 = (long long)tn * BN;
+    const int f0 = tn * (BN / 2);
 #pragma unroll
     for (int i = 0; i < LM; ++i) {
         const int piece = i * NT + tid;
         if constexpr (MA) {
             const int row = piece / 8, chunk = (piece % 8) ^ (row & 7);
-            const long long r = m0 + row < A.m.rows ? m0 + row : A.m.rows - 1;
+            const int r = m0 + row < A.m.rows ? row : (int)(A.m.rows - 1 - m0);
             mk[i] = chunk * (16 / ES);
-            mp[i] = (const char *)A.m.p + r * A.m.ld * ES + chunk * 16;
+            mo[i] = (unsigned)r * (unsigned)A.m.ld * ES + chunk * 16;
         } else {
             int row, col;
             across_of(piece, BM, row, col);
-            long long c = m0 + col;
-            if (c > A.m.width - 16 / ES) c = A.m.width - 16 / ES;
+            const long long last = A.m.width - 16 / ES - m0;
             mk[i] = row;
-            mp[i] = (const char *)A.m.p + c * ES;
+            mo[i] = (unsigned)row * (unsigned)A.m.ld * ES + (unsigned)(col < last ? col : (int)last) * ES;
         }
     }
 #pragma unroll
     for (int i = 0; i < LN; ++i) {
         const int piece = i * NT + tid;
         if constexpr (NA) {
-            const int row = piece / 8, chunk = (piece % 8) ^ (row & 7);
             constexpr int per = BN / WN, half = per / 2;
-            const int w = row / per, in = row % per;
-            int f = tn * (BN / 2) + w * half + in % half;
-            if (f >= A.F) f = A.F - 1;
+            const int row = piece / 8, chunk = (piece % 8) ^ (row & 7), in = row % per;
+            const int f = row / per * half + in % half, r = f0 + f < A.F ? f : A.F - 1 - f0;
             nk[i] = chunk * (16 / ES);
-            np[i] = (const char *)(in >= half ? A.n.p2 : A.n.p) + (long long)f * A.n.ld * ES + chunk * 16;
+            no[i] = (unsigned)r * (unsigned)A.n.ld * ES + chunk * 16;
         } else {
             int row, col;
             across_of(piece, BN, row, col);
-            long long c = (long long)tn * BN + col;
-            if (c > A.n.width - 16 / ES) c = A.n.width - 16 / ES;
+            const long long last = A.n.width - 16 / ES - n0;
             nk[i] = row;
-            np[i] = (const char *)0 + c * ES;
+            no[i] = (unsigned)row * (unsigned)A.n.ld * ES + (unsigned)(col < last ? col : (int)last) * ES;
         }
     }
+    const char *mb = (const char *)A.m.p + (MA ? m0 * A.m.ld : m0) * ES;
+    const long long m_step = MA ? ES : A.m.ld * ES, n_step = NA ? ES : A.n.ld * ES;  // bytes from one place along the sum to the next
+    const char *nb = (const char *)A.n.p + (NA ? (long long)f0 * A.n.ld : n0) * ES, *nb2 = nullptr;
+    if (ROLE != GATED_DW) nb2 = (const char *)A.n.p2 + (NA ? (long long)f0 * A.n.ld : n0) * ES;
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char *)smem;
     auto bring = [&](int step, int slot) {
         const int k0 = k_begin + step * KS;
         const unsigned to = lds0 + slot * STAGE + wave * 1024;
-#pragma unroll
-        for (int i = 0; i < LM; ++i) {
-            const void *src;
-            if constexpr (MA) src = mp[i] + (long long)k0 * ES;
-            else src = mp[i] + (long long)(k0 + mk[i]) * A.m.ld * ES;
-            if (k0 + mk[i] >= k_end) src = g_zeros;
-            dma16(src, to + i * NT * 16);
+        const char *m = mb + k0 * m_step, *n = nb + k0 * n_step, *n2 = nb2;
+        int f = k0;  // DX: the inner value (its sum runs over W_g's, then W_u's; both are padded to whole steps)
+        if constexpr (NA) n2 += k0 * n_step;
+        if constexpr (ROLE == GATED_DX) {
+            if (k0 >= A.Fp) f = k0 - A.Fp, n = nb2 + f * n_step;
         }
+        const bool whole = k0 + KS <= k_end && (ROLE != GATED_DX || f + KS <= A.F);
+        if (whole) {
 #pragma unroll
-        for (int i = 0; i < LN; ++i) {
-            const void *src;
-            if constexpr (NA) {
-                src = np[i] + (long long)k0 * ES;
-                if (k0 + nk[i] >= k_end) src = g_zeros;
-            } else if constexpr (ROLE == GATED_DX) {
-                const int k = k0 + nk[i];
-                const int f = k < A.Fp ? k : k - A.Fp;
-                src = (const char *)(k < A.Fp ? A.n.p : A.n.p2) + (long long)f * A.n.ld * ES + (size_t)np[i];
-                if (f >= A.F || k >= k_end) src = g_zeros;
-            } else {
-                src = (const char *)A.n.p + (long long)(k0 + nk[i]) * A.n.ld * ES + (size_t)np[i];
-                if (k0 + nk[i] >= k_end) src = g_zeros;
+            for (int i = 0; i < LM; ++i) dma16(m, mo[i], to + i * NT * 16);
+#pragma unroll
+            for (int i = 0; i < LN; ++i) {
+                // (which weight a piece is of is the same for the whole wave: 8 rows of 32 or 64)
+                const bool up = NA && __builtin_amdgcn_readfirstlane((i * NT + tid) / 8 % (BN / WN)) >= BN / WN / 2;
+                dma16(up ? n2 : n, no[i], to + BM * 128 + i * NT * 16);
             }
-            dma16(src, to + BM * 128 + i * NT * 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < LM; ++i) {
+                const void *src = m + mo[i];
+                if (k0 + mk[i] >= k_end) src = g_zeros;
+                dma16(src, to + i * NT * 16);
+            }
+#pragma unroll
+            for (int i = 0; i < LN; ++i) {
+                const bool up = NA && (i * NT + tid) / 8 % (BN / WN) >= BN / WN / 2;
+                const void *src = (up ? n2 : n) + no[i];
+                if (k0 + nk[i] >= k_end || (ROLE == GATED_DX && f + nk[i] >= A.F)) src = g_zeros;
+                dma16(src, to + BM * 128 + i * NT * 16);
+            }
         }
     };
     auto frag = [&](const char *tile, bool along, int cols, int t, int sub) -> F {
@@ -260,17 +274,11 @@ __global__ __launch_bounds__(64 * WM * WN) void tf_gated_kernel(GatedArgs A) {
     for (int i = 0; i < WTN; ++i)
 #pragma unroll
         for (int j = 0; j < WTM; ++j) acc[i][j] = o_f32x4{0.f, 0.f, 0.f, 0.f};
-    // A ring of stages: step s's loads go out STAGES - 1 steps before it, into the slot that step s - STAGES has left.
-    for (int s = 0; s < STAGES - 1; ++s)
-        if (s < steps) bring(s, s);
-    int slot = 0, next = STAGES - 1;
+    if (steps > 0) bring(0, 0);
     for (int s = 0; s < steps; ++s) {
-        if (s + STAGES - 2 < steps) stage_barrier<(STAGES - 2) * (LM + LN)>();
-        else stage_barrier<0>();
-        if (s + STAGES - 1 < steps) bring(s + STAGES - 1, next);
-        const char *tm_ = smem + slot * STAGE, *tn_ = tm_ + BM * 128;
-        slot = slot + 1 < STAGES ? slot + 1 : 0;
-        next = next + 1 < STAGES ? next + 1 : 0;
+        stage_barrier();
+        if (s + 1 < steps) bring(s + 1, (s + 1) & 1);
+        const char *tm_ = smem + (s & 1) * STAGE, *tn_ = tm_ + BM * 128;
         F fn[SUBS][WTN];
 #pragma unroll
         for (int i = 0; i < SUBS * WTN; ++i) fn[i / WTN][i % WTN] = frag(tn_, NA, BN, wn * WTN + i % WTN, i / WTN);
@@ -283,21 +291,22 @@ __global__ __launch_bounds__(64 * WM * WN) void tf_gated_kernel(GatedArgs A) {
     }
 
     typedef __attribute__((ext_vector_type(4))) E E4;
-    auto put = [&](E *p, bool vec, int left, o_f32x4 v) {  // up to `left` of four values
+    // Four values at any element's address: one access, whether it is aligned or not (rows of odd length: dh read value by
+    // value, or through LDS, cost a product of 5003 x 1032 -> 2731 36 us).
+    typedef E4 __attribute__((aligned(sizeof(E)))) E4u;
+    auto put = [&](E *p, int left, o_f32x4 v) {  // up to `left` of them
         const E4 e = __builtin_convertvector(v, E4);
-        if (vec && left >= 4) *(E4 *)p = e;
+        if (left >= 4) *(E4u *)p = e;
         else
             for (int i = 0; i < 4; ++i)
                 if (i < left) p[i] = e[i];
     };
     if constexpr (NA) {
         constexpr int HT = WTN / 2;
-        const bool vec = ROLE == GATED_D || (A.os % 4 == 0 && ((size_t)A.out & (4 * ES - 1)) == 0);
-        const bool dvec = ROLE == GATED_D && A.ds % 4 == 0 && ((size_t)A.dh & (4 * ES - 1)) == 0;
         struct Row {
             E4 g[HT];
         };
-        // dh's rows are read two tiles ahead of their use
+        // all of dh's tile is on its way before the first of it is used
         auto read = [&](int j) {
             Row r = {};
             if constexpr (ROLE == GATED_D) {
@@ -307,7 +316,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tf_gated_kernel(GatedArgs A) {
                 for (int i = 0; i < HT; ++i) {
                     const int f = tn * (BN / 2) + 16 * (wn * HT + i) + 4 * q;
                     const E *p = (const E *)A.dh + m * A.ds;
-                    if (dvec && f + 4 <= A.F) r.g[i] = *(const E4 *)(p + f);
+                    if (f + 4 <= A.F) r.g[i] = *(const E4u *)(p + f);
                     else
 #pragma unroll
                         for (int e = 0; e < 4; ++e) r.g[i][e] = p[f + e < A.F ? f + e : A.F - 1];
@@ -315,7 +324,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tf_gated_kernel(GatedArgs A) {
             }
             return r;
         };
-        in_turn<WTM, 3>(read, [&](int j, const Row &row) {
+        in_turn<WTM, WTM + 1>(read, [&](int j, const Row &row) {
             const long long m = m0 + 16 * (wm * WTM + j) + n;
             if (m >= A.M) return;
 #pragma unroll
@@ -330,7 +339,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tf_gated_kernel(GatedArgs A) {
                     v[e] = x, d[e] = y;
                 }
                 if constexpr (ROLE == GATED_H) {
-                    if (left > 0) put((E *)A.out + m * A.os + f, vec, left, v * b);
+                    if (left > 0) put((E *)A.out + m * A.os + f, left, v * b);
                 } else {
                     if (f >= A.Fp) continue;
                     const o_f32x4 g = __builtin_convertvector(row.g[i], o_f32x4);
@@ -339,13 +348,12 @@ __global__ __launch_bounds__(64 * WM * WN) void tf_gated_kernel(GatedArgs A) {
                     for (int e = 0; e < 4; ++e)  // the padding is zeros whatever the sums of the clamped rows are
                         if (e >= left) da[e] = db[e] = 0.0f;
                     E *o = (E *)A.out + m * A.os + f;
-                    put(o, true, 4, da);
-                    put(o + A.Fp, true, 4, db);
+                    put(o, 4, da);
+                    put(o + A.Fp, 4, db);
                 }
             }
         });
     } else {
-        const bool vec = A.os % 4 == 0 && ((size_t)A.out & (4 * ES - 1)) == 0 && (ROLE == GATED_DX || ((size_t)A.out2 & (4 * ES - 1)) == 0);
 #pragma unroll
         for (int j = 0; j < WTM; ++j) {
             const long long m = m0 + 16 * (wm * WTM + j) + n;
@@ -358,10 +366,10 @@ __global__ __launch_bounds__(64 * WM * WN) void tf_gated_kernel(GatedArgs A) {
                 if constexpr (SPLIT) {  // N is a multiple of 8
                     *(o_f32x4 *)(A.part + ((long long)blockIdx.y * A.M + m) * A.N + c) = acc[i][j];
                 } else if constexpr (ROLE == GATED_DX) {
-                    put((E *)A.out + m * A.os + c, vec, left, acc[i][j]);
+                    put((E *)A.out + m * A.os + c, left, acc[i][j]);
                 } else {
                     const int f = m < A.Fp ? (int)m : (int)m - A.Fp;
-                    if (f < A.F) put((E *)(m < A.Fp ? A.out : A.out2) + f * A.os + c, vec, left, acc[i][j]);
+                    if (f < A.F) put((E *)(m < A.Fp ? A.out : A.out2) + f * A.os + c, left, acc[i][j]);
                 }
             }
         }
@@ -461,30 +469,24 @@ tf_status gated_check(const tf_gated_config *c, int64_t n_rows) {
 }
 int64_t gated_pad(const tf_gated_config *c) { return ((int64_t)c->inner + 63) / 64 * 64; }
 
-// The tiles of a product of m x n, the first a wave's two-deep ring of 64 KB stages, the others of three and four: what
-// bounds a tile is its products (a quarter of them each time the tile's sides shrink to half, at 0.9 and 0.75 of the rate,
-// as the fragments' reads grow against them), and whole rounds of 256 compute units are paid for.
-struct Shape {
-    int m, n;
-};
-constexpr Shape kShapes[3] = {{256, 256}, {256, 128}, {128, 128}};
-constexpr double kShapeRate[3] = {1.0, 0.9, 0.75};
+// The tiles of a product of m x n: 256 x 256, one workgroup of eight waves a compute unit, or 128 x 128, two of four waves,
+// each with a ring of two stages.  Whole rounds of the compute units' tiles are paid for; a round of pairs of small tiles
+// takes 0.62 of one of large ones, for half its products.  5003 x 1032 with sums of 5504: 77 us in small tiles, 126 in
+// large ones; 256 x 128 with three stages and 128 x 128 with four, one workgroup a compute unit: 88 and 124.
+constexpr int kShapes[2] = {256, 128};
+constexpr double kRound[2] = {1.0, 0.62};
 int64_t gated_tiles(int64_t m, int64_t n, int shape) {
-    return ((m + kShapes[shape].m - 1) / kShapes[shape].m) * ((n + kShapes[shape].n - 1) / kShapes[shape].n);
+    const int b = kShapes[shape];
+    return ((m + b - 1) / b) * ((n + b - 1) / b);
 }
 int gated_shape(int64_t m, int64_t n) {
-    int best = 0;
-    double least = 0.0;
-    for (int i = 0; i < 3; ++i) {
-        const double t = (double)((gated_tiles(m, n, i) + 255) / 256) * kShapes[i].m * kShapes[i].n / kShapeRate[i];
-        if (i == 0 || t < least) best = i, least = t;
-    }
-    return best;
+    const int64_t large = gated_tiles(m, n, 0), small = gated_tiles(m, n, 1);
+    return (double)((large + 255) / 256) * kRound[0] <= (double)((small + 511) / 512) * kRound[1] ? 0 : 1;
 }
-// Parts of a sum of length k over `tiles` tiles of 128 x 128: as many as give every compute unit a workgroup,
+// Parts of a sum of length k over `tiles` tiles of 128 x 128: as many as give every compute unit two workgroups,
 // each at least 512 long (its products then take longer than its fp32 part's way out and back).
 int gated_parts(int64_t tiles, int64_t k) {
-    int64_t p = 256 / (tiles < 1 ? 1 : tiles);
+    int64_t p = 512 / (tiles < 1 ? 1 : tiles);
     if (p > k / 512) p = k / 512;
     if (p > 32) p = 32;
     return p < 1 ? 1 : (int)p;
@@ -497,8 +499,8 @@ struct GatedPlan {
 GatedPlan gated_plan(const tf_gated_config *c, int64_t m) {
     GatedPlan p = {};
     p.fp = gated_pad(c);
-    p.dx_parts = gated_parts(gated_tiles(m, c->width, 2), 2 * p.fp);
-    p.dw_parts = gated_parts(gated_tiles(2 * p.fp, c->width, 2), m);
+    p.dx_parts = gated_parts(gated_tiles(m, c->width, 1), 2 * p.fp);
+    p.dw_parts = gated_parts(gated_tiles(2 * p.fp, c->width, 1), m);
     p.dgu = ((size_t)m * 2 * p.fp * elem_bytes(c->elem) + 255) / 256 * 256;
     const size_t a = p.dx_parts > 1 ? (size_t)p.dx_parts * m * c->width * 4 : 0;
     const size_t b = p.dw_parts > 1 ? (size_t)p.dw_parts * 2 * p.fp * c->width * 4 : 0;
@@ -508,29 +510,25 @@ GatedPlan gated_plan(const tf_gated_config *c, int64_t m) {
 }
 
 template <class T, int ROLE, int SHAPE, bool GELU, bool SPLIT> void gated_tile(GatedArgs A, int parts, hipStream_t s) {
-    constexpr int BM = kShapes[SHAPE].m, BN = kShapes[SHAPE].n, WM = SHAPE == 1 ? 4 : 2, WN = SHAPE == 0 ? 4 : 2;
-    constexpr int STAGES = SHAPE + 2, LDS = STAGES * (BM + BN) * 128;
+    constexpr int BM = kShapes[SHAPE], BN = BM, WM = 2, WN = SHAPE == 0 ? 4 : 2, LDS = 2 * (BM + BN) * 128;
     constexpr int inner = ROLE == GATED_H || ROLE == GATED_D ? BN / 2 : BN;  // inner values of a tile
     A.tiles_m = (int)((A.M + BM - 1) / BM);
     A.tiles_n = (int)((A.N + inner - 1) / inner);
-    auto kernel = tf_gated_kernel<T, ROLE, BM, BN, WM, WN, STAGES, GELU, SPLIT>;
+    auto kernel = tf_gated_kernel<T, ROLE, BM, BN, WM, WN, GELU, SPLIT>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)A.tiles_m * A.tiles_n), SPLIT ? parts : 1), dim3(64 * WM * WN), LDS, s, A);
 }
 template <class T, int ROLE, bool GELU> void gated_product(const GatedArgs &A, int parts, hipStream_t s) {
     if constexpr (ROLE == GATED_DX || ROLE == GATED_DW) {
         if (parts > 1) {
-            gated_tile<T, ROLE, 2, GELU, true>(A, parts, s);
+            gated_tile<T, ROLE, 1, GELU, true>(A, parts, s);
             const int64_t blocks = (A.M * A.N / 4 + 255) / 256;
             hipLaunchKernelGGL((tf_gated_join_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, s, A.part, parts, A.M, A.N, A.F, A.Fp,
                                ROLE == GATED_DW, A.out, A.out2, A.os);
             return;
         }
     }
-    switch (gated_shape(A.M, ROLE == GATED_H || ROLE == GATED_D ? 2 * A.N : A.N)) {
-        case 0: gated_tile<T, ROLE, 0, GELU, false>(A, 1, s); break;
-        case 1: gated_tile<T, ROLE, 1, GELU, false>(A, 1, s); break;
-        default: gated_tile<T, ROLE, 2, GELU, false>(A, 1, s); break;
-    }
+    if (gated_shape(A.M, ROLE == GATED_H || ROLE == GATED_D ? 2 * A.N : A.N) == 0) gated_tile<T, ROLE, 0, GELU, false>(A, 1, s);
+    else gated_tile<T, ROLE, 1, GELU, false>(A, 1, s);
 }
 template <class T, bool BACK, bool GELU> void gated_project(const GatedArgs &A, hipStream_t s) {
     if (A.M <= kFewRows) {

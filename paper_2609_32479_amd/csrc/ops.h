@@ -12,7 +12,7 @@
 
 namespace {
 
-typedef __attribute__((ext_vector_type(2))) unsigned int o_u32x2;
+typedef __attribute__((ext_vector_type(2))) float o_f32x2;
 typedef __attribute__((ext_vector_type(4))) unsigned int o_u32x4;
 typedef __attribute__((ext_vector_type(4))) float o_f32x4;
 typedef __attribute__((ext_vector_type(8))) float o_f32x8;
