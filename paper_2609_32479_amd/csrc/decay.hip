@@ -286,6 +286,13 @@ __device__ __forceinline__ float sum16(float v) {
     v += dpp<0x140>(v);  // row_mirror
     return v;
 }
+// The sum over the four lanes n, n + 16, n + 32, n + 48, in all of them: halves, then rows of 16, swapped.
+__device__ __forceinline__ float sum_rows(float v) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
 // v summed over the lanes from `from` (this lane's own, at most this lane) to this one.
 __device__ __forceinline__ double sum_from(double v, int from, int lane) {
     const int in = lane & 15;
@@ -337,20 +344,24 @@ __device__ __forceinline__ int tile_of(int list, int w) { return list >> (2 * w)
 // 16 x 16 tiles on or below the diagonal dealt out to the waves, and pass through LDS; the last
 // wave prepares the next chunk's row sums meanwhile.  The next chunk's rows of the tensors are on their way to registers.
 template <class T, int DK, int DV, int MODE>
-__global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ? 4 : 3) : MODE == DECAY_OUT && DK * DV <= 64 * 64 ? 3 : 2) void tf_decay_span_kernel(DecayRuns R) {
+__global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ? 4 : 3) : DK * DV <= 32 * 32 || MODE == DECAY_OUT && DK * DV <= 64 * 64 ? 3 : 2) void tf_decay_span_kernel(DecayRuns R) {
     typedef typename MatOf<T>::M M;
     typedef typename M::E ME;
     typedef typename M::F F;
     constexpr bool OUT = MODE >= DECAY_OUT, DOT = MODE >= DECAY_DOT;
     constexpr int NT = span_threads(DV), NW = NT / 64, KM = M::KM, ES = sizeof(typename T::E);
-    constexpr int LK = DK + M::PAD, LV = DV + M::PAD, LP = kChunk + M::PAD;
+    constexpr int LK = DK + M::PAD, LV = DV + M::PAD;
+    // a row tile of the weights has columns up to its diagonal, in whole fragments
+    auto p_ld = [](int mt) { return (16 * mt + 16 + KM - 1) / KM * KM + M::PAD; };
+    auto p_at = [&](int mt) { return 16 * ((mt > 0 ? p_ld(0) : 0) + (mt > 1 ? p_ld(1) : 0) + (mt > 2 ? p_ld(2) : 0)); };
+    constexpr int PSIZE = 16 * (4 * M::PAD + (KM == 32 ? 192 : 160));
     constexpr int CT = 1, RG = DV == 32 ? 2 : 1, TM = 4 / RG;  // column tiles of a wave; waves that share them, and their row tiles
     constexpr int ST = DK / 16;                    // state tiles of a wave's column tile
     constexpr int NB = kChunk / KM;                // fragments along a chunk's rows
     constexpr int NS = parts_of<M>(DOT ? 3 : 2);   // parts of the state in its product with q
     constexpr int NU = parts_of<M>(3);             // parts of the weighted v in the state's update
     __shared__ __attribute__((aligned(16))) ME Qs[OUT ? kChunk * LK : 8], Ks[kChunk * LK], Vs[kChunk * LV],
-        Xs[DOT ? kChunk * LV : 8], Ps[OUT ? kChunk * LP : 8];
+        Xs[DOT ? kChunk * LV : 8], Ps[OUT ? PSIZE : 8];
     __shared__ ChunkRows rows_of[2];
     __shared__ int wild[2];
     __shared__ float rowp[DOT ? 4 : 1][kChunk], colp[DOT ? 4 : 1][kChunk], dots[DOT ? NW / RG : 1][kChunk];
@@ -500,7 +511,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         fetch_rows(1);
     }
     if (OUT)  // the weights above the diagonal that share a fragment with some below
-        for (int i = tid; i < kChunk * LP * (int)sizeof(ME) / 4; i += NT) ((unsigned *)Ps)[i] = 0;
+        for (int i = tid; i < PSIZE * (int)sizeof(ME) / 4; i += NT) ((unsigned *)Ps)[i] = 0;
     __syncthreads();
     put(0);
     __syncthreads();
@@ -511,10 +522,14 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         const bool slow = __builtin_amdgcn_readfirstlane(wild[c & 1]);
         fetch(c + 1);
         F vf[NB][CT];  // the wave's columns of v, for the state and for the output
-#pragma unroll
-        for (int k = 0; k < NB; ++k)
+        auto read_v = [&](int k) {
 #pragma unroll
             for (int j = 0; j < CT; ++j) vf[k][j] = M::down(Vs, LV, k * KM, c0 + 16 * j, n, q);
+        };
+        if (OUT) {
+#pragma unroll
+            for (int k = 0; k < NB; ++k) read_v(k);
+        }
         // the last wave prepares the next chunk's rows while the others compute the weights
         if (wave == NW - 1 && c + 1 < chunks) {
             put_rows(rows_of[(c + 1) & 1], c + 1);
@@ -529,12 +544,17 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                 const int t = 16 * mt + n, s = 16 * ms + 4 * q, f = seg_first(W.seg[t]);
                 const bool apart = seg_first(__builtin_amdgcn_readfirstlane(W.seg[16 * mt])) >= 16 * ms + 16;  // all of the tile's rows are of later sequences
                 typedef __attribute__((ext_vector_type(4))) ME V4;
-                o_f32x4 a = {0.f, 0.f, 0.f, 0.f};
+                o_f32x4 a = {0.f, 0.f, 0.f, 0.f}, z = {0.f, 0.f, 0.f, 0.f};
                 if (!apart) {
                     struct Two { F k, q; };
                     in_turn<DK / KM, (DK / KM < 4 ? DK / KM + 1 : 4)>(
                         [&](int i) { return Two{M::along(Ks, LK, 16 * ms + n, i * KM, q), M::along(Qs, LK, 16 * mt + n, i * KM, q)}; },
                         [&](int, Two f) { a = M::mma(f.k, f.q, a); });
+                    if (pairs) {
+#pragma unroll
+                        for (int k0 = 0; k0 < DV; k0 += KM)
+                            z = M::mma(M::along(Vs, LV, 16 * ms + n, k0, q), M::along(Xs, LV, 16 * mt + n, k0, q), z);
+                    }
                     const float th = W.bh[t], tl = W.bl[t];
                     const o_f32x4 sh = *(const o_f32x4 *)&W.bh[s], sl = *(const o_f32x4 *)&W.bl[s];
 #pragma unroll
@@ -543,23 +563,16 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                         a[i] = s + i <= t && s + i >= f ? a[i] * (e * sc) : 0.0f;
                     }
                 }
-                *(V4 *)(Ps + t * LP + s) = __builtin_convertvector(a, V4);
+                *(V4 *)(Ps + p_at(mt) + n * p_ld(mt) + s) = __builtin_convertvector(a, V4);
                 if (pairs) {
                     // products of dq's weights with q k: their sums by t and by s are what q dq and k dk have of them
-                    o_f32x4 z = {0.f, 0.f, 0.f, 0.f};
-                    if (!apart) {
-#pragma unroll
-                        for (int k0 = 0; k0 < DV; k0 += KM)
-                            z = M::mma(M::along(Vs, LV, 16 * ms + n, k0, q), M::along(Xs, LV, 16 * mt + n, k0, q), z);
-                    }
                     float row = 0.0f;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         z[i] = s + i <= t && s + i >= f ? a[i] * z[i] : 0.0f;
                         row += z[i];
                     }
-                    row += __shfl_xor(row, 16);
-                    row += __shfl_xor(row, 32);
+                    row = sum_rows(row);
                     if (q == 0) rowp[ms][t] = row;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) z[i] = sum16(z[i]);
@@ -606,6 +619,9 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                                                      M::template split<NS>(x, sp[j]);
                                                  }
                                              }
+                                             // (a branch costs more than the bf16 products of rows that are not the sequence's)
+                                             const int t = 16 * row_tile(m);
+                                             if (KM == 16 && (t + 16 <= a || t >= b)) return;
 #pragma unroll
                                              for (int e = NS - 1; e >= 0; --e)
 #pragma unroll
@@ -636,6 +652,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
 #pragma unroll
                     for (int k = 0; k < NB; ++k) {
                         if (k * KM + KM <= a || k * KM >= b) continue;
+                        if (!OUT) read_v(k);
                         F vp[CT][NU];
                         float w[KM / 4];
 #pragma unroll
@@ -696,21 +713,25 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
 #pragma unroll
                         for (int i = 0; i < 4; ++i) z += o[j][m][i] * x[i];
                     }
-                    z += __shfl_xor(z, 16);
-                    z += __shfl_xor(z, 32);
+                    z = sum_rows(z);
                     if (q == 0) dots[group][16 * row_tile(m) + n] = z;
                 }
             }
             if (!slow) {
+                int from[TM];  // the first row that a row tile has weights of
+#pragma unroll
+                for (int m = 0; m < TM; ++m)
+                    from[m] = KM == 16 ? seg_first(__builtin_amdgcn_readfirstlane(W.seg[16 * row_tile(m)])) : 0;
                 in_turn<NB * TM, 4>(
                     [&](int i) {
                         F f = {};
-                        if (i / TM * KM <= 16 * row_tile(i % TM)) f = M::along(Ps, LP, 16 * row_tile(i % TM) + n, i / TM * KM, q);
+                        const int mt = row_tile(i % TM);
+                        if (i / TM * KM <= 16 * mt) f = M::along(Ps + p_at(mt), p_ld(mt), n, i / TM * KM, q);
                         return f;
                     },
                     [&](int i, F f) {
                         const int k = i / TM, m = i % TM;
-                        if (k * KM <= 16 * row_tile(m)) {
+                        if (k * KM <= 16 * row_tile(m) && (KM == 32 || k * KM + KM > from[m])) {
 #pragma unroll
                             for (int j = 0; j < CT; ++j) o[j][m] = M::mma(vf[k][j], f, o[j][m]);
                         }
@@ -725,7 +746,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                         for (int j = 0; j < CT; ++j)
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
-                                o[j][m][i] += (float)Ps[t * LP + s] * (float)Vs[s * LV + c0 + 16 * j + 4 * q + i];
+                                o[j][m][i] += (float)Ps[p_at(row_tile(m)) + n * p_ld(row_tile(m)) + s] * (float)Vs[s * LV + c0 + 16 * j + 4 * q + i];
                 }
             }
             // (the chunk's first row is a scalar; 64 rows of a stride fit in 32 bits)

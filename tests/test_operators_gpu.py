@@ -146,32 +146,29 @@ def test_rows_outside_of_sequences_and_strided_rows(tf, dtype):
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_infinities_stay_in_their_sequence(tf, dtype, bad):
     """NaN or infinity in one row: the other sequences' outputs and gradients, and the earlier rows of its own, are
-    those without it."""
+    within their bounds of the 64-bit form without it.  (A chunk with such a row multiplies one by one instead of on the
+    matrix cores, so that its sums' last digits differ from those without it; both have the bounds, which count the
+    roundings of either order.)"""
     lengths = [17, 40, 9, 90]
     t, off, rows = _attn_inputs(9, dtype, lengths, 2, 2, 32, 64)
     o = torch.from_numpy(off).cuda()
+    fwd, back = _ref(t, off, 32 ** -0.5), _ref(t, off, 32 ** -0.5, d_out=t["d_out"].double())
+    ref = {**fwd, **back}
+    bound = {k: forms.attention_bound(k, dtype, ref[k], max(lengths)) for k in ref}
+    at = 30                      # in the second sequence (rows 17 .. 56)
     for name in ("q", "k", "v", "d_out", "g"):
         if name == "g" and bad == float("inf"):
             continue
-        at = 30                      # in the second sequence (rows 17 .. 56)
-        clean = _cuda(t)
-        dirty = _cuda(t)
-        dirty[name][at] = bad
-        run = lambda c: (tf.decay_attention(c["q"], c["k"], c["v"], c["g"], o, return_state=True),  # noqa: E731
-                         tf.decay_attention_backward(c["d_out"], c["q"], c["k"], c["v"], c["g"], o))
-        (a, sa), ga = run(clean)
-        (b, sb), gb = run(dirty)
-        # (a chunk with such a row multiplies one by one instead of on the matrix cores: the sums' last digits differ)
-        tol = 4 * forms.HALF[dtype]
-        near = lambda x, y, what: torch.testing.assert_close(x.float(), y.float(), rtol=tol, atol=tol * 8, msg=lambda m: f"{name} {what}: {m}")  # noqa: E731
-        near(a[:17], b[:17], "out before")
-        near(a[57:], b[57:], "out after")
-        near(a[17:at], b[17:at], "out earlier rows")
+        c = _cuda(t)
+        c[name][at] = bad
+        out, last = tf.decay_attention(c["q"], c["k"], c["v"], c["g"], o, return_state=True)
+        got = dict(zip(("dq", "dk", "dv", "dg"), tf.decay_attention_backward(c["d_out"], c["q"], c["k"], c["v"], c["g"], o)))
+        for n, x in {"out": out, **got}.items():
+            for rows_of, what in ((slice(0, 17), "before"), (slice(57, rows), "after")):
+                _within(f"{name}: {n} {what}", x[rows_of], ref[n][0][rows_of], bound[n][rows_of])
+        _within(f"{name}: earlier rows", out[17:at], ref["out"][0][17:at], bound["out"][17:at])
         for i in (0, 2, 3):
-            near(sa[i], sb[i], "state")
-        for x, y, what in zip(ga[:4], gb[:4], ("dq", "dk", "dv", "dg")):
-            near(x[:17], y[:17], what)
-            near(x[57:], y[57:], what)
+            _within(f"{name}: state", last[i], ref["state"][0][i], bound["state"][i])
 
 
 def test_forgetting_rows_part_a_sequence(tf):
