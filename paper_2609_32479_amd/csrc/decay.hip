@@ -189,9 +189,9 @@ struct DecayRun {
     Spans spans;
 };
 
-// A launch's runs: one, or two of the same shapes side by side (blockIdx.y).
+// A launch's runs: one, or up to three of the same shapes side by side (blockIdx.y).
 struct DecayRuns {
-    DecayRun run[2];
+    DecayRun run[3];
 };
 
 enum { DECAY_STATE = 0, DECAY_OUT = 1, DECAY_DOT = 2 };
@@ -367,7 +367,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
     __shared__ float rowp[DOT ? 4 : 1][kChunk], colp[DOT ? 4 : 1][kChunk], dots[DOT ? NW / RG : 1][kChunk];
 
     const DecayRun &A = R.run[blockIdx.y];
-    const bool pairs = MODE == DECAY_DOT && A.pairs;
+    const bool dot = DOT && A.x, pairs = DOT && A.pairs;
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int n = lane % 16, q = lane / 16, group = wave / RG, rg = wave % RG, c0 = 16 * CT * group;
     auto row_tile = [&](int m) { return RG == 1 ? m : rg ? 1 + m : 3 * m; };  // (pairs of tiles with equally long sums)
@@ -455,7 +455,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
     if (OUT) bq = (const char *)A.q + ((long long)lo * A.qs + h / A.qg * DK) * ES;
     const char *bk = (const char *)A.k + ((long long)lo * A.ks + h / A.kg * DK) * ES;
     const char *bv = (const char *)A.v + ((long long)lo * A.vs + h / A.vg * DV) * ES;
-    if (DOT) bx = (const char *)A.x + ((long long)lo * A.xs + h / A.xg * DV) * ES;
+    if (dot) bx = (const char *)A.x + ((long long)lo * A.xs + h / A.xg * DV) * ES;
     auto chunk_rows = [&](int at) { return at < 0 || at >= hi - lo ? 0 : hi - lo - at < kChunk ? hi - lo - at : kChunk; };
     auto chunk_at = [&](int c) { return (dir > 0 ? c : chunks - 1 - c) * kChunk; };  // the c-th on the way: its first row in memory, from lo
     auto fetch = [&](int c) {
@@ -463,7 +463,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         if (OUT) tq.load(bq + (long long)at * A.qs * ES, A.qs, rows, tid);
         tk.load(bk + (long long)at * A.ks * ES, A.ks, rows, tid);
         tv.load(bv + (long long)at * A.vs * ES, A.vs, rows, tid);
-        if (DOT) tx.load(bx + (long long)at * A.xs * ES, A.xs, rows, tid);
+        if (dot) tx.load(bx + (long long)at * A.xs * ES, A.xs, rows, tid);
     };
     // The last wave's: a chunk's sequences and decays, one row a lane.
     int2 next_seq = {0, 0};
@@ -500,7 +500,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         if (OUT) tq.store(Qs, rows, dir, tid);
         tk.store(Ks, rows, dir, tid);
         tv.store(Vs, rows, dir, tid);
-        if (DOT) tx.store(Xs, rows, dir, tid);
+        if (dot) tx.store(Xs, rows, dir, tid);
         if (tk.infinite() || tv.infinite()) wild[c & 1] = 1;
     };
     fetch(0);
@@ -702,7 +702,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
             }
         }
         if (OUT) {
-            if (DOT) {
+            if (dot) {
 #pragma unroll
                 for (int m = 0; m < TM; ++m) {
                     float z = 0.0f;
@@ -768,7 +768,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         __syncthreads();
         if (tid == 0) wild[c & 1] = 0;
         put(c + 1);
-        if (DOT && wave == 0) {
+        if (dot && wave == 0) {
             const int t = lane;
             if (t < rows) {
                 float z = 0.0f;
@@ -1033,10 +1033,17 @@ __global__ __launch_bounds__(64) void tf_decay_sum_kernel(const float *__restric
 }
 
 // Gradients of queries and keys that several heads share: the heads' own, added in order.
+struct DecayShare {
+    const float *part[2];  // dq, dk
+    void *out[2];
+    long long stride[2];
+};
 template <class T>
-__global__ __launch_bounds__(256) void tf_decay_share_kernel(const float *__restrict__ part, int group, int shared, int width,
-                                                             long long n_rows, const int32_t *__restrict__ offsets, int n_seqs,
-                                                             typename T::E *__restrict__ out, long long stride, const int *bad) {
+__global__ __launch_bounds__(256) void tf_decay_share_kernel(DecayShare S, int group, int shared, int width, long long n_rows,
+                                                             const int32_t *__restrict__ offsets, int n_seqs, const int *bad) {
+    const float *part = blockIdx.y ? S.part[1] : S.part[0];
+    typename T::E *out = (typename T::E *)(blockIdx.y ? S.out[1] : S.out[0]);
+    const long long stride = blockIdx.y ? S.stride[1] : S.stride[0];
     const int per = shared * width / 4;
     const bool wrong = any_bad(bad);
     const long long lo = wrong ? 0 : offsets[0], hi = wrong ? n_rows : offsets[n_seqs];
@@ -1208,18 +1215,15 @@ void empty_run(const int32_t *offsets, int n_seqs, long long size, const float *
                        p.bad);
 }
 template <class T>
-void share_one(const float *part, const tf_decay_config *c, int64_t n_rows, const int32_t *offsets, int n_seqs, void *out,
-               int64_t stride, const int *bad, hipStream_t s) {
+void share_one(const DecayShare &S, const tf_decay_config *c, int64_t n_rows, const int32_t *offsets, int n_seqs, const int *bad, hipStream_t s) {
     const int64_t items = n_rows * c->n_qk_heads * c->d_k / 4, blocks = (items + 255) / 256;
-    hipLaunchKernelGGL((tf_decay_share_kernel<T>), dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, s, part,
-                       c->n_heads / c->n_qk_heads, (int)c->n_qk_heads, (int)c->d_k, (long long)n_rows, offsets, n_seqs,
-                       (typename T::E *)out, (long long)stride, bad);
+    hipLaunchKernelGGL((tf_decay_share_kernel<T>), dim3((unsigned)(blocks < 8192 ? blocks : 8192), 2), dim3(256), 0, s, S,
+                       c->n_heads / c->n_qk_heads, (int)c->n_qk_heads, (int)c->d_k, (long long)n_rows, offsets, n_seqs, bad);
 }
-void share_run(const float *part, const tf_decay_config *c, int64_t n_rows, const int32_t *offsets, int n_seqs, void *out,
-               int64_t stride, const int *bad, hipStream_t s) {
-    if (c->elem == TF_ELEM_BF16) share_one<ElemBF16>(part, c, n_rows, offsets, n_seqs, out, stride, bad, s);
-    else if (c->elem == TF_ELEM_FP32) share_one<ElemF32>(part, c, n_rows, offsets, n_seqs, out, stride, bad, s);
-    else share_one<ElemF16>(part, c, n_rows, offsets, n_seqs, out, stride, bad, s);
+void share_run(const DecayShare &S, const tf_decay_config *c, int64_t n_rows, const int32_t *offsets, int n_seqs, const int *bad, hipStream_t s) {
+    if (c->elem == TF_ELEM_BF16) share_one<ElemBF16>(S, c, n_rows, offsets, n_seqs, bad, s);
+    else if (c->elem == TF_ELEM_FP32) share_one<ElemF32>(S, c, n_rows, offsets, n_seqs, bad, s);
+    else share_one<ElemF16>(S, c, n_rows, offsets, n_seqs, bad, s);
 }
 
 bool decay_sizes_ok(const tf_decay_config *c, int64_t n_rows, int32_t n_seqs) {
@@ -1280,7 +1284,7 @@ extern "C" tf_status tf_decay_attention(const tf_decay_config *c, const void *q,
         A.out_scale = c->scale, A.kv_scale = 1.0f;
         A.offsets = offsets, A.n_seqs = n_seqs, A.heads = c->n_heads, A.dir = c->reverse ? -1 : 1, A.bad = p.bad;
         A.spans = {p.info, (int)n_rows, decay_span(c, n_rows), (int)decay_spans(c, n_rows)};
-        const DecayRuns R = {{A, A}};
+        const DecayRuns R = {{A}};
         chain_run(c->elem, R, 1, c->d_k, c->d_v, stream);
         span_run(c->elem, R, 1, c->d_k, c->d_v, DECAY_OUT, stream);
     }
@@ -1348,16 +1352,20 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
         K.x = k, K.xs = k_stride, K.xg = group;
         K.out = shared ? (void *)p.dk : dk, K.os = shared ? (int64_t)H * c->d_k : dk_stride, K.out_f32 = shared;
         K.turned = 1, K.db = p.db;
-        span_run(c->elem, {{Q, K}}, 2, c->d_v, c->d_k, DECAY_DOT, stream);
         // dv, and the initial states' gradients
         DecayRun V = B;
         V.q = k, V.qs = k_stride, V.qg = group;
         V.out = dv, V.os = dv_stride;
         V.sf = d_initial, V.sf_decay = 1;
-        span_run(c->elem, {{V, V}}, 1, c->d_k, c->d_v, DECAY_OUT, stream);
+        if (c->d_k == c->d_v) {  // (apart they took 63 and 27 us for 9.6 thousand rows, which leave compute units idle)
+            V.x = nullptr;
+            span_run(c->elem, {{Q, K, V}}, 3, c->d_k, c->d_v, DECAY_DOT, stream);
+        } else {
+            span_run(c->elem, {{Q, K}}, 2, c->d_v, c->d_k, DECAY_DOT, stream);
+            span_run(c->elem, {{V}}, 1, c->d_k, c->d_v, DECAY_OUT, stream);
+        }
         if (shared) {
-            share_run(p.dq, c, n_rows, offsets, n_seqs, dq, dq_stride, p.bad, stream);
-            share_run(p.dk, c, n_rows, offsets, n_seqs, dk, dk_stride, p.bad, stream);
+            share_run({{p.dq, p.dk}, {dq, dk}, {dq_stride, dk_stride}}, c, n_rows, offsets, n_seqs, p.bad, stream);
         }
     }
     DecayGrad G = {};
