@@ -478,8 +478,9 @@ size_t tf_decay_backward_workspace_size(const tf_decay_config *cfg, int64_t n_ro
 /*
  * q, k           device, [n_rows][n_qk_heads][d_k].
  * v              device, [n_rows][n_heads][d_v].
- * log_decay      device, float32: rows of n_heads, decay_stride apart, or with
- *                decay_stride 0 one value a head for all rows.
+ * log_decay      device, float32 (at any float's address): rows of n_heads,
+ *                decay_stride apart, or with decay_stride 0 one value a head for
+ *                all rows.
  * offsets        device, int32 [n_seqs + 1]: sequence i owns rows offsets[i] ..
  *                offsets[i+1]-1, as for fit_tracks.  Offsets that decrease or
  *                leave [0, n_rows] set TF_SEQ_BAD_OFFSETS in *flags and make
@@ -582,7 +583,8 @@ tf_status tf_qk_norm_rotate_backward(const tf_qk_norm_config *cfg, const void *d
  * [inner][width], h [n_rows][inner].  SiLU a / (1 + exp(-a)), GELU a Phi(a).
  * Sums in fp32 (fp32 tensors: products by the fp32 matrix instruction); the
  * activation and the product in fp32, one rounding at the store.
- * Supported: width a multiple of 8, any inner, both up to 2^20.
+ * Supported: width a multiple of 8, any inner, both up to 2^20, row strides of x, the
+ * weights and their gradients up to 2^22, up to 2^28 rows.
  */
 typedef enum { TF_ACT_SILU = 0, TF_ACT_GELU = 1 } tf_activation;
 

@@ -1117,6 +1117,7 @@ int decay_span(const tf_decay_config *c, int64_t n_rows) {
     int64_t s = n_rows * c->n_heads / (c->d_k * c->d_v > 64 * 64 ? 512 : 1024) / kChunk * kChunk;
     if (s < kMinSpan) s = kMinSpan;
     if (s > 512) s = 512;
+    if (n_rows <= 2 * kMinSpan) s = 2 * kMinSpan;  // one span: no state to pass, two launches less
     return (int)s;
 }
 int64_t decay_spans(const tf_decay_config *c, int64_t n_rows) {
@@ -1266,7 +1267,9 @@ extern "C" tf_status tf_decay_attention(const tf_decay_config *c, const void *q,
     if (n_seqs == 0) return TF_OK;
     if (!offsets || !workspace) return TF_EINVAL;
     if (n_rows > 0 && (!q || !k || !v || !out || !log_decay)) return TF_EINVAL;
-    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || ((uintptr_t)workspace & 255)) return TF_EINVAL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(initial_state) || !aligned16(final_state) ||
+        ((uintptr_t)workspace & 255))
+        return TF_EINVAL;
     const Plan p = decay_plan(c, n_rows, n_seqs, false, false, workspace);
     if (workspace_bytes < p.bytes) return TF_EINVAL;
     index_run(offsets, n_seqs, n_rows, p, flags, stream);
@@ -1312,7 +1315,7 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
     if (!offsets || !workspace || (!decay_stride && !d_log_decay)) return TF_EINVAL;
     if (n_rows > 0 && (!q || !k || !v || !d_out || !dq || !dk || !dv || !log_decay || !d_log_decay)) return TF_EINVAL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(d_out) || !aligned16(dq) || !aligned16(dk) ||
-        !aligned16(dv) || ((uintptr_t)workspace & 255))
+        !aligned16(dv) || !aligned16(initial_state) || !aligned16(d_state) || !aligned16(d_initial) || ((uintptr_t)workspace & 255))
         return TF_EINVAL;
     const Plan p = decay_plan(c, n_rows, n_seqs, true, d_state != nullptr, workspace);
     if (workspace_bytes < p.bytes) return TF_EINVAL;

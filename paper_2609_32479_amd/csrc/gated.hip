@@ -27,6 +27,7 @@
 #include "ops.h"
 
 #include <cmath>
+#include <initializer_list>
 
 namespace {
 
@@ -467,6 +468,13 @@ tf_status gated_check(const tf_gated_config *c, int64_t n_rows) {
     if (c->width % 8 || c->width > (1 << 20) || c->inner > (1 << 20) || n_rows > (1 << 28)) return TF_EUNSUPPORTED;
     return TF_OK;
 }
+// A tile's rows are addressed by 32-bit offsets, its workgroups by 31-bit numbers.
+bool gated_fits(const tf_gated_config *c, int64_t n_rows, std::initializer_list<int64_t> strides) {
+    for (int64_t s : strides)
+        if (s > (1 << 22)) return false;
+    const int64_t inner = (c->inner + 63) / 64, rows = (n_rows + 127) / 128, width = (c->width + 127) / 128;
+    return inner * rows <= INT32_MAX && 2 * inner * width <= INT32_MAX && rows * width <= INT32_MAX;
+}
 int64_t gated_pad(const tf_gated_config *c) { return ((int64_t)c->inner + 63) / 64 * 64; }
 
 // The tiles of a product of m x n: 256 x 256, one workgroup of eight waves a compute unit, or 128 x 128, two of four waves,
@@ -558,6 +566,7 @@ extern "C" tf_status tf_gated_ffn(const tf_gated_config *c, const void *x, int64
     const tf_status st = gated_check(c, n_rows);
     if (st != TF_OK) return st;
     if (!stride_ok(x_stride, c->width, c->elem) || !stride_ok(w_stride, c->width, c->elem) || out_stride < c->inner) return TF_EINVAL;
+    if (!gated_fits(c, n_rows, {x_stride, w_stride})) return TF_EUNSUPPORTED;
     if (n_rows == 0) return TF_OK;
     if (!x || !w_gate || !w_up || !out) return TF_EINVAL;
     if (!aligned16(x) || !aligned16(w_gate) || !aligned16(w_up) || ((uintptr_t)out & (elem_bytes(c->elem) - 1))) return TF_EINVAL;
@@ -586,6 +595,7 @@ extern "C" tf_status tf_gated_ffn_backward(const tf_gated_config *c, const void 
     if (!stride_ok(x_stride, c->width, c->elem) || !stride_ok(w_stride, c->width, c->elem) || !stride_ok(dx_stride, c->width, c->elem) ||
         !stride_ok(dw_stride, c->width, c->elem) || d_out_stride < c->inner)
         return TF_EINVAL;
+    if (!gated_fits(c, n_rows, {x_stride, w_stride, dx_stride, dw_stride})) return TF_EUNSUPPORTED;
     if (!w_gate || !w_up || !dw_gate || !dw_up || !workspace) return TF_EINVAL;
     if (n_rows > 0 && (!d_out || !x || !dx)) return TF_EINVAL;
     if (!aligned16(x) || !aligned16(w_gate) || !aligned16(w_up) || !aligned16(dx) || !aligned16(dw_gate) || !aligned16(dw_up) ||

@@ -88,31 +88,30 @@ def _check(status: int, what: str):
 
 @functools.lru_cache(maxsize=256)
 def _config(kind, *fields):
-    """A configuration of these plain values (read only: the library takes it by pointer)."""
-    return kind(*fields)
+    """A configuration of these plain values and a pointer to it (the library only reads it)."""
+    cfg = kind(*fields)
+    return cfg, ctypes.byref(cfg)
 
 
 class _On:
     """The tensor's device, with ``stream`` as its current stream; entering gives the stream's handle."""
-    __slots__ = ("stack", "handle")
+    __slots__ = ("tensor", "stream", "stack")
 
     def __init__(self, tensor: torch.Tensor, stream):
-        index = tensor.get_device()
-        if stream is None and index == torch.cuda.current_device():  # nothing to switch
-            self.stack, self.handle = None, torch._C._cuda_getCurrentRawStream(index)
-            return
+        self.tensor, self.stream, self.stack = tensor, stream, None
+
+    def __enter__(self) -> int:
+        index, stream = self.tensor.get_device(), self.stream
+        if stream is None and index == torch._C._cuda_getDevice():  # nothing to switch
+            return torch._C._cuda_getCurrentRawStream(index)
         self.stack = contextlib.ExitStack()
         self.stack.enter_context(torch.cuda.device(index))
         if stream is None:
-            self.handle = int(torch.cuda.current_stream().cuda_stream)
-            return
+            return int(torch.cuda.current_stream().cuda_stream)
         if not hasattr(stream, "cuda_stream"):
             stream = torch.cuda.ExternalStream(int(stream))
         self.stack.enter_context(torch.cuda.stream(stream))
-        self.handle = int(stream.cuda_stream)
-
-    def __enter__(self) -> int:
-        return self.handle
+        return int(stream.cuda_stream)
 
     def __exit__(self, *exc):
         if self.stack is not None:
@@ -127,7 +126,7 @@ def _same(name: str, x, like: torch.Tensor, dtype=None):
         raise ValueError(f"{name} must be a GPU tensor")
     if x.get_device() != like.get_device():
         raise ValueError(f"{name} is on {x.device}, the others on {like.device}")
-    if dtype is not None and x.dtype != dtype:
+    if dtype is not None and x.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, not {x.dtype}")
 
 
@@ -147,14 +146,14 @@ def _rows3(name: str, x: torch.Tensor, like: torch.Tensor, rows=None, heads=None
             (width is not None and shape[2] != width):
         want = ", ".join("?" if v is None else str(v) for v in (rows, heads, width))
         raise ValueError(f"{name} must have shape [{want}], not {list(shape)}")
-    r, h, w = shape
+    _, h, w = shape
     n = h * w
     if x.is_contiguous():
         return n
     sr, sh, sw = x.stride()
     if (w > 1 and sw != 1) or (h > 1 and sh != w):
         raise ValueError(f"{name}'s rows [heads, width] must be contiguous")
-    if r <= 1:
+    if shape[0] <= 1:
         return n  # (one row: any stride)
     if sr < n:
         raise ValueError(f"{name}'s rows overlap")
@@ -164,7 +163,7 @@ def _rows3(name: str, x: torch.Tensor, like: torch.Tensor, rows=None, heads=None
 def _new(name: str, x, like: torch.Tensor, shape, dtype) -> torch.Tensor:
     """The output tensor: a new one, or the caller's, checked to be contiguous."""
     if x is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
     _same(name, x, like, dtype)
     if tuple(x.shape) != tuple(shape) or not x.is_contiguous():
         raise ValueError(f"{name} must be contiguous with shape {list(shape)}")
@@ -174,7 +173,7 @@ def _new(name: str, x, like: torch.Tensor, shape, dtype) -> torch.Tensor:
 def _rows_out(name: str, x, like: torch.Tensor, shape):
     """The output rows (new, or the caller's, which may be strided) and their stride."""
     if x is None:
-        return torch.empty(shape, dtype=like.dtype, device=like.device), shape[1] * shape[2]
+        return like.new_empty(shape), shape[1] * shape[2]
     return x, _rows3(name, x, like, *shape)
 
 
@@ -187,7 +186,7 @@ def _offsets(offsets, like: torch.Tensor) -> int:
 
 def _workspace(ws, need: int, like: torch.Tensor) -> torch.Tensor:
     if ws is None:
-        return torch.empty(max(need, 256), dtype=torch.uint8, device=like.device)
+        return like.new_empty((max(need, 256),), dtype=torch.uint8)
     _same("workspace", ws, like)
     if not ws.is_contiguous() or ws.numel() * ws.element_size() < need:
         raise ValueError(f"workspace must be contiguous and hold {need} bytes")
@@ -257,7 +256,7 @@ def decay_attention(q, k, v, log_decay, offsets, scale=None, reverse=False, init
     is OR-ed with SEQ_BAD_OFFSETS when the offsets make no sequences (the outputs are
     NaN then).
     """
-    cfg, (qs, ks, vs) = _decay_inputs(q, k, v, scale, reverse)
+    (cfg, at), (qs, ks, vs) = _decay_inputs(q, k, v, scale, reverse)
     rows, n = q.shape[0], _offsets(offsets, q)
     gs = _decays(log_decay, q, rows, cfg.n_heads)
     _state("initial_state", initial_state, q, n, cfg.n_heads, cfg.d_k, cfg.d_v)
@@ -266,9 +265,9 @@ def decay_attention(q, k, v, log_decay, offsets, scale=None, reverse=False, init
         out, os = _rows_out("out", out, q, (rows, cfg.n_heads, cfg.d_v))
         if return_state or final_state is not None:
             final_state = _new("final_state", final_state, q, (n, cfg.n_heads, cfg.d_k, cfg.d_v), torch.float32)
-        ws = _workspace(workspace, int(_lib().tf_decay_workspace_size(ctypes.byref(cfg), rows)), q)
+        ws = _workspace(workspace, int(_lib().tf_decay_workspace_size(at, rows)), q)
         _check(_lib().tf_decay_attention(
-            ctypes.byref(cfg), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, log_decay.data_ptr(), gs, rows,
+            at, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, log_decay.data_ptr(), gs, rows,
             offsets.data_ptr(), n, _ptr(initial_state), ws.data_ptr(), _bytes(ws), out.data_ptr(), os, _ptr(final_state),
             _ptr(flags), s), "tf_decay_attention")
     return out, final_state
@@ -282,7 +281,7 @@ def decay_attention_backward(d_out, q, k, v, log_decay, offsets, scale=None, rev
     d_out as out, d_state as the last states (None: they are not used), the other
     arguments those of the forward call.  d_initial is None without an initial_state.
     """
-    cfg, (qs, ks, vs) = _decay_inputs(q, k, v, scale, reverse)
+    (cfg, at), (qs, ks, vs) = _decay_inputs(q, k, v, scale, reverse)
     rows, n, h = q.shape[0], _offsets(offsets, q), cfg.n_heads
     gs = _decays(log_decay, q, rows, h)
     _state("initial_state", initial_state, q, n, h, cfg.d_k, cfg.d_v)
@@ -296,10 +295,10 @@ def decay_attention_backward(d_out, q, k, v, log_decay, offsets, scale=None, rev
         d_log_decay = _new("d_log_decay", d_log_decay, q, tuple(log_decay.shape), torch.float32)
         if initial_state is not None or d_initial is not None:
             d_initial = _new("d_initial", d_initial, q, (n, h, cfg.d_k, cfg.d_v), torch.float32)
-        need = int(_lib().tf_decay_backward_workspace_size(ctypes.byref(cfg), rows, n, int(d_state is not None)))
+        need = int(_lib().tf_decay_backward_workspace_size(at, rows, n, int(d_state is not None)))
         ws = _workspace(workspace, need, q)
         _check(_lib().tf_decay_attention_backward(
-            ctypes.byref(cfg), d_out.data_ptr(), ds, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
+            at, d_out.data_ptr(), ds, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
             log_decay.data_ptr(), gs, rows, offsets.data_ptr(), n, _ptr(initial_state), _ptr(d_state), ws.data_ptr(),
             _bytes(ws), dq.data_ptr(), dqs, dk.data_ptr(), dks, dv.data_ptr(), dvs, d_log_decay.data_ptr(),
             _ptr(d_initial), _ptr(flags), s), "tf_decay_attention_backward")
@@ -311,7 +310,7 @@ def decay_attention_step(q, k, v, log_decay, state, scale=None, state_out=None, 
     d_v], log_decay [n, heads] or [heads], state float32 [n, heads, d_k, d_v].
     Returns (out [n, heads, d_v], the new states).  ``state_out`` may be ``state``,
     which is then updated in place; by default the new states are a new tensor."""
-    cfg, (qs, ks, vs) = _decay_inputs(q, k, v, scale, False)
+    (cfg, at), (qs, ks, vs) = _decay_inputs(q, k, v, scale, False)
     n = q.shape[0]
     gs = _decays(log_decay, q, n, cfg.n_heads)
     if state is None:
@@ -319,9 +318,10 @@ def decay_attention_step(q, k, v, log_decay, state, scale=None, state_out=None, 
     _state("state", state, q, n, cfg.n_heads, cfg.d_k, cfg.d_v)
     with _on(q, stream) as s:
         out, os = _rows_out("out", out, q, (n, cfg.n_heads, cfg.d_v))
-        state_out = _new("state_out", state_out, q, tuple(state.shape), torch.float32)
+        if state_out is not state:  # (in place: checked above)
+            state_out = _new("state_out", state_out, state, state.shape, torch.float32)
         _check(_lib().tf_decay_attention_step(
-            ctypes.byref(cfg), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, log_decay.data_ptr(), gs, n,
+            at, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, log_decay.data_ptr(), gs, n,
             state.data_ptr(), state_out.data_ptr(), out.data_ptr(), os, s), "tf_decay_attention_step")
     return out, state_out
 
@@ -361,12 +361,12 @@ def qk_norm_rotate(q, k, q_gain, k_gain, offsets=None, positions=None, rotary_di
     With offsets only the sequences' rows are written.  ``q_out`` and ``k_out`` may be
     q and k.
     """
-    cfg, qs, ks, n = _norm_inputs(q, k, q_gain, k_gain, offsets, positions, rotary_dim, base, interleaved, eps)
+    (cfg, at), qs, ks, n = _norm_inputs(q, k, q_gain, k_gain, offsets, positions, rotary_dim, base, interleaved, eps)
     with _on(q, stream) as s:
         q_out, qos = _rows_out("q_out", q_out, q, tuple(q.shape))
         k_out, kos = _rows_out("k_out", k_out, q, tuple(k.shape))
         _check(_lib().tf_qk_norm_rotate(
-            ctypes.byref(cfg), q.data_ptr(), qs, k.data_ptr(), ks, q.shape[0], q_gain.data_ptr(), k_gain.data_ptr(),
+            at, q.data_ptr(), qs, k.data_ptr(), ks, q.shape[0], q_gain.data_ptr(), k_gain.data_ptr(),
             _ptr(positions), _ptr(offsets), n, q_out.data_ptr(), qos, k_out.data_ptr(), kos, s), "tf_qk_norm_rotate")
     return q_out, k_out
 
@@ -377,7 +377,7 @@ def qk_norm_rotate_backward(dq_out, dk_out, q, k, q_gain, k_gain, offsets=None, 
     """Gradients of qk_norm_rotate's inputs from those of its outputs: (dq, dk,
     dq_gain, dk_gain); q, k and the rest as in the forward call.  ``dq`` and ``dk``
     may be ``dq_out`` and ``dk_out``."""
-    cfg, qs, ks, n = _norm_inputs(q, k, q_gain, k_gain, offsets, positions, rotary_dim, base, interleaved, eps)
+    (cfg, at), qs, ks, n = _norm_inputs(q, k, q_gain, k_gain, offsets, positions, rotary_dim, base, interleaved, eps)
     rows, d = q.shape[0], q.shape[2]
     dqos = _rows3("dq_out", dq_out, q, *q.shape)
     dkos = _rows3("dk_out", dk_out, q, *k.shape)
@@ -386,9 +386,9 @@ def qk_norm_rotate_backward(dq_out, dk_out, q, k, q_gain, k_gain, offsets=None, 
         dk, dks = _rows_out("dk", dk, q, tuple(k.shape))
         dq_gain = _new("dq_gain", dq_gain, q, (d,), torch.float32)
         dk_gain = _new("dk_gain", dk_gain, q, (d,), torch.float32)
-        ws = _workspace(workspace, int(_lib().tf_qk_norm_workspace_size(ctypes.byref(cfg), rows)), q)
+        ws = _workspace(workspace, int(_lib().tf_qk_norm_workspace_size(at, rows)), q)
         _check(_lib().tf_qk_norm_rotate_backward(
-            ctypes.byref(cfg), dq_out.data_ptr(), dqos, dk_out.data_ptr(), dkos, q.data_ptr(), qs, k.data_ptr(), ks, rows,
+            at, dq_out.data_ptr(), dqos, dk_out.data_ptr(), dkos, q.data_ptr(), qs, k.data_ptr(), ks, rows,
             q_gain.data_ptr(), k_gain.data_ptr(), _ptr(positions), _ptr(offsets), n, ws.data_ptr(), _bytes(ws),
             dq.data_ptr(), dqs, dk.data_ptr(), dks, dq_gain.data_ptr(), dk_gain.data_ptr(), s), "tf_qk_norm_rotate_backward")
     return dq, dk, dq_gain, dk_gain
@@ -425,12 +425,12 @@ def gated_ffn(x, w_gate, w_up, activation="silu", out=None, stream=None):
     """act(x w_gate^T) * (x w_up^T) in one kernel: x [rows, width], both weights
     [inner, width], of one type (fp32, bf16, fp16); activation "silu" or "gelu" (a
     Phi(a)).  Returns [rows, inner]."""
-    cfg, xs, ws = _gated_inputs(x, w_gate, w_up, activation)
+    (cfg, at), xs, ws = _gated_inputs(x, w_gate, w_up, activation)
     with _on(x, stream) as s:
         if out is None:
-            out = torch.empty((x.shape[0], cfg.inner), dtype=x.dtype, device=x.device)
+            out = x.new_empty((x.shape[0], cfg.inner))
         os = _matrix("out", out, x, x.shape[0], cfg.inner)
-        _check(_lib().tf_gated_ffn(ctypes.byref(cfg), x.data_ptr(), xs, x.shape[0], w_gate.data_ptr(), w_up.data_ptr(), ws,
+        _check(_lib().tf_gated_ffn(at, x.data_ptr(), xs, x.shape[0], w_gate.data_ptr(), w_up.data_ptr(), ws,
                                    out.data_ptr(), os, s), "tf_gated_ffn")
     return out
 
@@ -439,7 +439,7 @@ def gated_ffn_backward(d_out, x, w_gate, w_up, activation="silu", dx=None, dw_ga
                        stream=None):
     """Gradients of gated_ffn's inputs: (dx, dw_gate, dw_up).  The projections are
     computed again from x and the weights."""
-    cfg, xs, ws = _gated_inputs(x, w_gate, w_up, activation)
+    (cfg, at), xs, ws = _gated_inputs(x, w_gate, w_up, activation)
     rows = x.shape[0]
     ds = _matrix("d_out", d_out, x, rows, cfg.inner)
     with _on(x, stream) as s:
@@ -450,9 +450,9 @@ def gated_ffn_backward(d_out, x, w_gate, w_up, activation="silu", dx=None, dw_ga
         dws = _matrix("dw_gate", dw_gate, x, *w_gate.shape)
         if _matrix("dw_up", dw_up, x, *w_up.shape) != dws:
             raise ValueError("dw_gate and dw_up must have the same row stride")
-        wk = _workspace(workspace, int(_lib().tf_gated_ffn_workspace_size(ctypes.byref(cfg), rows)), x)
+        wk = _workspace(workspace, int(_lib().tf_gated_ffn_workspace_size(at, rows)), x)
         _check(_lib().tf_gated_ffn_backward(
-            ctypes.byref(cfg), d_out.data_ptr(), ds, x.data_ptr(), xs, rows, w_gate.data_ptr(), w_up.data_ptr(), ws,
+            at, d_out.data_ptr(), ds, x.data_ptr(), xs, rows, w_gate.data_ptr(), w_up.data_ptr(), ws,
             wk.data_ptr(), _bytes(wk), dx.data_ptr(), dxs, dw_gate.data_ptr(), dw_up.data_ptr(), dws, s),
             "tf_gated_ffn_backward")
     return dx, dw_gate, dw_up

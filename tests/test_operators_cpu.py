@@ -41,6 +41,12 @@ def test_decay_attention_refusals(tf):
                 dict(out=A + 8)):
         assert _attn(tf, ok, **bad) == tf.TF_EINVAL, bad
     assert _attn(tf, ok, rows=2 ** 31 - 1) == tf.TF_EUNSUPPORTED
+    assert _attn(tf, ok, qs=(1 << 24) + 8) == tf.TF_EUNSUPPORTED
+    L = tf.lib()
+    for i in (12, 17):   # states off their alignment
+        args = [ctypes.byref(ok), A, 128, A, 128, A, 128, A, 4, 100, A, 3, None, A, 1 << 40, A, 128, None, None, None]
+        args[i] = A + 4
+        assert L.tf_decay_attention(*args) == tf.TF_EINVAL
     L = tf.lib()
     assert L.tf_decay_workspace_size(ctypes.byref(ok), 100) > 0
     assert L.tf_decay_workspace_size(ctypes.byref(ok), -1) == 0
@@ -110,6 +116,9 @@ def test_gated_refusals(tf):
     for bad in (dict(elem=5), dict(width=0), dict(inner=0), dict(act=2), dict(act=-1)):
         assert run(cfg(**bad)) == tf.TF_EINVAL, bad
     assert run(cfg(width=100), xs=104, ws=104) == tf.TF_EUNSUPPORTED
+    assert run(cfg(), xs=(1 << 22) + 8) == tf.TF_EUNSUPPORTED
+    assert run(cfg(inner=1 << 20), rows=1 << 28, os_=1 << 20) == tf.TF_EUNSUPPORTED
+    assert run(cfg(), rows=(1 << 28) + 1) == tf.TF_EUNSUPPORTED
     for bad in (dict(rows=-1), dict(xs=120), dict(xs=132), dict(ws=64), dict(os_=99), dict(x=None), dict(x=A + 8), dict(out=A + 1)):
         assert run(cfg(), **bad) == tf.TF_EINVAL, bad
     assert L.tf_gated_ffn_workspace_size(ctypes.byref(cfg()), 10) >= 10 * 2 * 128 * 2

@@ -95,6 +95,22 @@ def test_attention_and_its_gradients(tf, dtype, shape, lengths, reverse, states)
         _within(name, x, want, bound)
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("first,last", [(True, False), (False, True)])
+@pytest.mark.parametrize("dk,dv", [(32, 32), (64, 32)])
+def test_attention_states_on_one_side(tf, dtype, first, last, dk, dv):
+    """An initial state without the last one's gradient, and the other way round; sequences of one row and of 200."""
+    t, off, rows = _attn_inputs(29, dtype, [200, 1, 0, 199, 1], 2, 2, dk, dv)
+    c, o, scale = _cuda(t), torch.from_numpy(off).cuda(), dk ** -0.5
+    ref = _ref(t, off, scale, s0=t["s0"].double() if first else None, d_out=t["d_out"].double(),
+               d_state=t["d_state"].double() if last else None)
+    mine = torch.full_like(c["s0"], -7.0)
+    got = tf.decay_attention_backward(c["d_out"], c["q"], c["k"], c["v"], c["g"], o, initial_state=c["s0"] if first else None,
+                                      d_state=c["d_state"] if last else None, d_initial=mine)
+    for name, x in zip(("dq", "dk", "dv", "dg", "d_initial"), got):
+        _within(name, x, ref[name][0], forms.attention_bound(name, dtype, ref[name], 200))
+
+
 def test_attention_gradients_against_differences(tf):
     """fp32: the loss's slope along random directions, by central differences of the 64-bit form."""
     t, off, rows = _attn_inputs(5, FP32, [9, 0, 70, 1], 2, 1, 32, 32)
