@@ -166,7 +166,7 @@ struct Spans {
 struct DecayRun {
     const void *q, *k, *v, *x;           // x: what the part from the state is multiplied with for db
     long long qs, ks, vs, xs;            // row strides, elements
-    int qg, kg, vg, xg;                  // heads that share one of these
+    int group, qg, kg, vg, xg;           // heads that share a query's and key's; whether q, k, v, x are one
     void *out;
     long long os;
     int out_f32;                         // out holds fp32 rows of all heads (summed over sharing heads later)
@@ -208,15 +208,14 @@ template <class T, class M, int D, int NT> struct Tile {
     typedef typename M::E ME;
     static constexpr int VEC = 16 / sizeof(E), PIECES = D / VEC, STEP = NT / PIECES, N = (kChunk + STEP - 1) / STEP;
     o_u32x4 raw[N];
+    // (through a descriptor that ends behind the chunk's last row, so that rows past it come as zeros: a load under a condition
+    // is waited for where its register meets the other value, four memory latencies a chunk)
     __device__ __forceinline__ void load(const void *base, long long stride, int rows, int tid) {
-        const int p = tid / PIECES;
-        const unsigned at = (unsigned)(p * (int)stride + tid % PIECES * VEC) * (unsigned)sizeof(E);
+        const unsigned row = (unsigned)stride * (unsigned)sizeof(E);
+        const auto all = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)((rows - 1) * row + D * (unsigned)sizeof(E)), 0x00020000);
+        const unsigned at = tid / PIECES * row + tid % PIECES * 16u;
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const char *b = (const char *)base + (long long)j * STEP * stride * (long long)sizeof(E);
-            raw[j] = o_u32x4{0, 0, 0, 0};
-            if (p + j * STEP < rows) raw[j] = *(const o_u32x4 *)(b + at);
-        }
+        for (int j = 0; j < N; ++j) raw[j] = __builtin_amdgcn_raw_buffer_load_b128(all, (int)(at + j * STEP * row), 0, 0);
     }
     __device__ __forceinline__ void store(ME *lds, int rows, int dir, int tid) const {
 #pragma unroll
@@ -452,11 +451,12 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
     Tile<T, M, DV, NT> tv, tx;
     // the head's columns, at the span's first row
     const char *bq = nullptr, *bx = nullptr;
-    if (OUT) bq = (const char *)A.q + ((long long)lo * A.qs + h / A.qg * DK) * ES;
-    const char *bk = (const char *)A.k + ((long long)lo * A.ks + h / A.kg * DK) * ES;
-    const char *bv = (const char *)A.v + ((long long)lo * A.vs + h / A.vg * DV) * ES;
-    if (dot) bx = (const char *)A.x + ((long long)lo * A.xs + h / A.xg * DV) * ES;
-    auto chunk_rows = [&](int at) { return at < 0 || at >= hi - lo ? 0 : hi - lo - at < kChunk ? hi - lo - at : kChunk; };
+    const int hs = h / A.group;
+    if (OUT) bq = (const char *)A.q + ((long long)lo * A.qs + (A.qg ? hs : h) * DK) * ES;
+    const char *bk = (const char *)A.k + ((long long)lo * A.ks + (A.kg ? hs : h) * DK) * ES;
+    const char *bv = (const char *)A.v + ((long long)lo * A.vs + (A.vg ? hs : h) * DV) * ES;
+    if (dot) bx = (const char *)A.x + ((long long)lo * A.xs + (A.xg ? hs : h) * DV) * ES;
+    auto chunk_rows = [&](int at) { return hi - lo - at < kChunk ? hi - lo - at : kChunk; };
     auto chunk_at = [&](int c) { return (dir > 0 ? c : chunks - 1 - c) * kChunk; };  // the c-th on the way: its first row in memory, from lo
     auto fetch = [&](int c) {
         const int at = chunk_at(c), rows = chunk_rows(at);
@@ -471,7 +471,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
     double total = 0.0;
     auto fetch_rows = [&](int c) {
         const int at = chunk_at(c), rows = chunk_rows(at), i = lane < rows ? lane : 0;
-        const int r = rows ? lo + at + (dir > 0 ? i : rows - 1 - i) : lo;
+        const int r = lo + at + (dir > 0 ? i : rows - 1 - i);
         next_seq = A.spans.info[r];
         int rg = A.shift ? r - dir : r;  // (where that is another sequence's it is not used)
         rg = rg < olo ? olo : rg >= ohi ? ohi - 1 : rg;
@@ -508,7 +508,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
     if (wave == NW - 1) {
         fetch_rows(0);
         put_rows(rows_of[0], 0);
-        fetch_rows(1);
+        if (chunks > 1) fetch_rows(1);
     }
     if (OUT)  // the weights above the diagonal that share a fragment with some below
         for (int i = tid; i < PSIZE * (int)sizeof(ME) / 4; i += NT) ((unsigned *)Ps)[i] = 0;
@@ -520,7 +520,11 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         const int at = chunk_at(c), rows = chunk_rows(at);
         const ChunkRows &W = rows_of[c & 1];
         const bool slow = __builtin_amdgcn_readfirstlane(wild[c & 1]);
-        fetch(c + 1);
+        // (behind the last chunk there is nothing to fetch; a large state's kernel is better off without the branch, loading
+        // that chunk again: tracks' gradients at 32 columns, fp32, 301 us with the branch and 318 without, long sequences'
+        // outputs at 128 columns, bf16, 174 us with it and 167 without)
+        if (DK * DV > 64 * 64) fetch(c + 1 < chunks ? c + 1 : c);
+        else if (c + 1 < chunks) fetch(c + 1);
         F vf[NB][CT];  // the wave's columns of v, for the state and for the output
         auto read_v = [&](int k) {
 #pragma unroll
@@ -533,7 +537,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         // the last wave prepares the next chunk's rows while the others compute the weights
         if (wave == NW - 1 && c + 1 < chunks) {
             put_rows(rows_of[(c + 1) & 1], c + 1);
-            fetch_rows(c + 2);
+            if (c + 2 < chunks) fetch_rows(c + 2);
         }
         if (OUT) {
             // weights: tile (s tile ms, t tile mt), transposed, so that four consecutive s of a row t land in a lane
@@ -767,7 +771,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         }
         __syncthreads();
         if (tid == 0) wild[c & 1] = 0;
-        put(c + 1);
+        if (c + 1 < chunks) put(c + 1);
         if (dot && wave == 0) {
             const int t = lane;
             if (t < rows) {
@@ -1279,7 +1283,7 @@ extern "C" tf_status tf_decay_attention(const tf_decay_config *c, const void *q,
         DecayRun A = {};
         const int group = c->n_heads / c->n_qk_heads;
         A.q = q, A.k = k, A.v = v, A.qs = q_stride, A.ks = k_stride, A.vs = v_stride;
-        A.qg = A.kg = group, A.vg = 1, A.xg = 1;
+        A.group = group, A.qg = A.kg = 1;
         A.out = out, A.os = out_stride;
         A.g = log_decay, A.gs = decay_stride;
         A.s0 = initial_state, A.sf = final_state;
@@ -1324,40 +1328,40 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
     index_run(offsets, n_seqs, n_rows, p, flags, stream);
     if (n_seqs > 0 && d_initial) empty_run(offsets, n_seqs, states, d_state, d_initial, p, stream);
     DecayRun A = {};
-    A.g = log_decay, A.gs = decay_stride;
+    A.group = group, A.g = log_decay, A.gs = decay_stride;
     A.offsets = offsets, A.n_seqs = n_seqs, A.heads = H, A.bad = p.bad;
     A.spans = {p.info, (int)n_rows, decay_span(c, n_rows), (int)decay_spans(c, n_rows)};
     if (n_rows > 0 && n_seqs > 0) {
         // the states at the spans' ends, and their gradients
         DecayRun F = A;
-        F.k = k, F.ks = k_stride, F.kg = group, F.v = v, F.vs = v_stride, F.vg = 1, F.qg = F.xg = 1;
+        F.k = k, F.ks = k_stride, F.kg = 1, F.v = v, F.vs = v_stride;
         F.s0 = initial_state, F.dir = dir, F.out_scale = F.kv_scale = 1.0f;
         F.local = p.local[0], F.mult = p.mult[0], F.kind = p.kind[0];
         DecayRun B = A;
-        B.k = q, B.ks = q_stride, B.kg = group, B.v = d_out, B.vs = d_out_stride, B.vg = 1, B.qg = B.xg = 1;
+        B.k = q, B.ks = q_stride, B.kg = 1, B.v = d_out, B.vs = d_out_stride;
         B.s0 = d_state, B.dir = -dir, B.shift = 1, B.out_scale = 1.0f, B.kv_scale = c->scale;
         B.local = p.local[1], B.mult = p.mult[1], B.kind = p.kind[1];
         chain_run(c->elem, {{F, B}}, 2, c->d_k, c->d_v, stream);
         const bool shared = group > 1;
         // dq
         DecayRun Q = F;
-        Q.q = d_out, Q.qs = d_out_stride, Q.qg = 1;
-        Q.k = v, Q.ks = v_stride, Q.kg = 1;
-        Q.v = k, Q.vs = k_stride, Q.vg = group;
-        Q.x = q, Q.xs = q_stride, Q.xg = group;
+        Q.q = d_out, Q.qs = d_out_stride, Q.qg = 0;
+        Q.k = v, Q.ks = v_stride, Q.kg = 0;
+        Q.v = k, Q.vs = k_stride, Q.vg = 1;
+        Q.x = q, Q.xs = q_stride, Q.xg = 1;
         Q.out = shared ? (void *)p.dq : dq, Q.os = shared ? (int64_t)H * c->d_k : dq_stride, Q.out_f32 = shared;
         Q.turned = 1, Q.sf = p.sl, Q.db = p.da, Q.pairs = 1, Q.out_scale = c->scale, Q.kv_scale = 1.0f;
         // dk
         DecayRun K = B;
-        K.q = v, K.qs = v_stride, K.qg = 1;
-        K.k = d_out, K.ks = d_out_stride, K.kg = 1;
-        K.v = q, K.vs = q_stride, K.vg = group;
-        K.x = k, K.xs = k_stride, K.xg = group;
+        K.q = v, K.qs = v_stride, K.qg = 0;
+        K.k = d_out, K.ks = d_out_stride, K.kg = 0;
+        K.v = q, K.vs = q_stride, K.vg = 1;
+        K.x = k, K.xs = k_stride, K.xg = 1;
         K.out = shared ? (void *)p.dk : dk, K.os = shared ? (int64_t)H * c->d_k : dk_stride, K.out_f32 = shared;
         K.turned = 1, K.db = p.db;
         // dv, and the initial states' gradients
         DecayRun V = B;
-        V.q = k, V.qs = k_stride, V.qg = group;
+        V.q = k, V.qs = k_stride, V.qg = 1;
         V.out = dv, V.os = dv_stride;
         V.sf = d_initial, V.sf_decay = 1;
         if (c->d_k == c->d_v) {  // (apart they took 63 and 27 us for 9.6 thousand rows, which leave compute units idle)
