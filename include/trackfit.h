@@ -437,7 +437,8 @@ tf_status tf_mingru_device_error(const tf_mingru *h, hipStream_t stream, int32_t
  * Tensors are row-major with unit stride inside a row ([heads][width] of a row are
  * contiguous); row strides are in elements.  Pointers of tensors and workspaces and
  * the rows' strides in bytes are multiples of 16 (workspaces of tf_decay_*: 256);
- * anything else is TF_EINVAL.  Outputs must not overlap inputs unless said so.
+ * anything else is TF_EINVAL.  Outputs must not overlap inputs or each other unless
+ * said so; one that starts where an input does is TF_EINVAL.
  * All calls: TF_EINVAL (null pointers that are needed, negative sizes, strides
  * below a row's width, alignment, unknown element type, a workspace that is too
  * small), TF_EUNSUPPORTED (sizes outside the supported set), TF_EHIP.
@@ -455,7 +456,8 @@ typedef enum { TF_ELEM_FP32 = 0, TF_ELEM_BF16 = 1, TF_ELEM_FP16 = 2 } tf_elem;
  * consecutive heads; values, decays, states and outputs have n_heads.
  * Log decays are meant to be <= 0; below about -104 (-inf too) a row forgets all
  * before it.  reverse = 1: t runs from each sequence's last row to its first.
- * Supported: d_k and d_v 32, 64 or 128, up to 1024 heads, row strides up to 2^24.
+ * Supported: d_k and d_v 32, 64 or 128, up to 1024 heads, row strides up to 2^24, up
+ * to 2^31 - 2^16 rows and sequences; a single step: fewer than 2^24 states.
  * fp32 tensors: products and sums in fp32.  bf16: states, decays and sums in fp32;
  * the weights exp(b_t - b_s) q_t k_s of the values inside a chunk of 64 rows are
  * rounded to bf16.  fp16: as fp32, rounded once at the store.
@@ -531,7 +533,8 @@ tf_status tf_decay_attention_step(const tf_decay_config *cfg, const void *q, int
  * for pairs j < rotary_dim / 2: values j and j + rotary_dim / 2, or (interleaved)
  * 2 j and 2 j + 1.  Values from rotary_dim on are only normalised.
  * Sums and products in fp32, angles in fp64, one rounding at the store (16-bit
- * types: sines and cosines good to 2^-20).
+ * types: sines and cosines good to 2^-20); a head's sum of squares has to be within
+ * fp32's range.
  * Supported: head_dim 32, 64, 128 or 256, rotary_dim a multiple of 16 up to it, up to
  * 1024 heads of each, row strides up to 2^22.
  */

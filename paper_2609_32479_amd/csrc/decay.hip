@@ -1232,8 +1232,8 @@ void share_run(const DecayShare &S, const tf_decay_config *c, int64_t n_rows, co
 }
 
 bool decay_sizes_ok(const tf_decay_config *c, int64_t n_rows, int32_t n_seqs) {
-    // rows are 32-bit numbers, and so are workgroups
-    return n_rows <= INT32_MAX - 2048 && decay_spans(c, n_rows) * c->n_heads < INT32_MAX;
+    // rows and sequences are 32-bit numbers (with room for the last step of the index's loops), and so are a launch's threads
+    return n_rows <= INT32_MAX - 2048 && n_seqs <= INT32_MAX - 512 * kCheckers && decay_spans(c, n_rows) * c->n_heads < 1 << 24;
 }
 
 // A chunk's rows are addressed by 32-bit offsets.
@@ -1274,6 +1274,8 @@ extern "C" tf_status tf_decay_attention(const tf_decay_config *c, const void *q,
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(initial_state) || !aligned16(final_state) ||
         ((uintptr_t)workspace & 255))
         return TF_EINVAL;
+    if (n_rows > 0 && over_inputs({out}, {q, k, v, log_decay})) return TF_EINVAL;
+    if (over_inputs({out, final_state}, {initial_state})) return TF_EINVAL;
     const Plan p = decay_plan(c, n_rows, n_seqs, false, false, workspace);
     if (workspace_bytes < p.bytes) return TF_EINVAL;
     index_run(offsets, n_seqs, n_rows, p, flags, stream);
@@ -1321,6 +1323,8 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(d_out) || !aligned16(dq) || !aligned16(dk) ||
         !aligned16(dv) || !aligned16(initial_state) || !aligned16(d_state) || !aligned16(d_initial) || ((uintptr_t)workspace & 255))
         return TF_EINVAL;
+    if (n_rows > 0 && over_inputs({dq, dk, dv, d_log_decay}, {d_out, q, k, v, log_decay})) return TF_EINVAL;
+    if (n_seqs > 0 && over_inputs({d_initial}, {initial_state, d_state})) return TF_EINVAL;
     const Plan p = decay_plan(c, n_rows, n_seqs, true, d_state != nullptr, workspace);
     if (workspace_bytes < p.bytes) return TF_EINVAL;
     const int H = c->n_heads, group = H / c->n_qk_heads, dir = c->reverse ? -1 : 1, size = c->d_k * c->d_v;
@@ -1402,11 +1406,12 @@ extern "C" tf_status tf_decay_attention_step(const tf_decay_config *c, const voi
     if (!stride_ok(q_stride, qw, c->elem) || !stride_ok(k_stride, qw, c->elem) || !stride_ok(v_stride, vw, c->elem) ||
         !stride_ok(out_stride, vw, c->elem))
         return TF_EINVAL;
-    if ((int64_t)n_seqs * c->n_heads > INT32_MAX) return TF_EUNSUPPORTED;
+    if ((int64_t)n_seqs * c->n_heads >= 1 << 24) return TF_EUNSUPPORTED;  // a launch has fewer than 2^32 threads
     if (n_seqs == 0) return TF_OK;
     if (!q || !k || !v || !log_decay || !state || !state_out || !out) return TF_EINVAL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(state) || !aligned16(state_out))
         return TF_EINVAL;
+    if (over_inputs({out}, {q, k, v, log_decay, state}) || over_inputs({state_out}, {q, k, v, log_decay})) return TF_EINVAL;
     const dim3 grid((unsigned)((int64_t)n_seqs * c->n_heads));
     const int group = c->n_heads / c->n_qk_heads;
 #define TF_STEP(T)                                                                                                               \

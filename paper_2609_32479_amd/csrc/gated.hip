@@ -27,7 +27,6 @@
 #include "ops.h"
 
 #include <cmath>
-#include <initializer_list>
 
 namespace {
 
@@ -570,6 +569,7 @@ extern "C" tf_status tf_gated_ffn(const tf_gated_config *c, const void *x, int64
     if (n_rows == 0) return TF_OK;
     if (!x || !w_gate || !w_up || !out) return TF_EINVAL;
     if (!aligned16(x) || !aligned16(w_gate) || !aligned16(w_up) || ((uintptr_t)out & (elem_bytes(c->elem) - 1))) return TF_EINVAL;
+    if (over_inputs({out}, {x, w_gate, w_up})) return TF_EINVAL;
     GatedArgs A = {};
     A.m = {x, nullptr, x_stride, (int)n_rows, c->width};
     A.n = {w_gate, w_up, w_stride, c->inner, c->width};
@@ -600,6 +600,8 @@ extern "C" tf_status tf_gated_ffn_backward(const tf_gated_config *c, const void 
     if (n_rows > 0 && (!d_out || !x || !dx)) return TF_EINVAL;
     if (!aligned16(x) || !aligned16(w_gate) || !aligned16(w_up) || !aligned16(dx) || !aligned16(dw_gate) || !aligned16(dw_up) ||
         !aligned16(workspace) || ((uintptr_t)d_out & (elem_bytes(c->elem) - 1)))
+        return TF_EINVAL;
+    if ((n_rows > 0 && over_inputs({dx, dw_gate, dw_up}, {d_out, x})) || over_inputs({dx, dw_gate, dw_up}, {w_gate, w_up}) || dw_gate == dw_up)
         return TF_EINVAL;
     const GatedPlan p = gated_plan(c, n_rows);
     if (workspace_bytes < p.bytes) return TF_EINVAL;

@@ -7,6 +7,7 @@
 
 #include <cstddef>
 #include <cstdint>
+#include <initializer_list>
 
 #include "trackfit.h"
 
@@ -46,7 +47,7 @@ template <typename T> __device__ __forceinline__ void store8(typename T::E *p, o
 __device__ __forceinline__ int seq_of_row(const int32_t *__restrict__ offsets, int n, long long r) {
     int lo = 0, hi = n;  // offsets[lo - 1] <= r < offsets[hi], where these exist
     while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
+        const int mid = lo + ((hi - lo) >> 1);
         if (offsets[mid] <= r) lo = mid + 1;
         else hi = mid;
     }
@@ -76,6 +77,14 @@ inline bool elem_ok(int e) { return e == TF_ELEM_FP32 || e == TF_ELEM_BF16 || e 
 // A row stride in elements that keeps 16-byte accesses of an aligned array aligned.
 inline bool stride_ok(int64_t stride, int64_t width, int e) {
     return stride >= width && (stride * (int64_t)elem_bytes(e)) % 16 == 0;
+}
+
+// Whether an output is one of the inputs: workgroups would read what others have written.
+inline bool over_inputs(std::initializer_list<const void *> outputs, std::initializer_list<const void *> inputs) {
+    for (const void *o : outputs)
+        for (const void *i : inputs)
+            if (o && o == i) return true;
+    return false;
 }
 
 }  // namespace

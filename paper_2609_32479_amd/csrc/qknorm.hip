@@ -20,7 +20,6 @@
 #include "ops.h"
 
 #include <cmath>
-#include <initializer_list>
 
 namespace {
 
@@ -328,6 +327,11 @@ bool strides_fit(std::initializer_list<int64_t> strides) {
     return true;
 }
 
+// An output that starts at its input but whose rows lie elsewhere.
+bool in_place_elsewhere(const void *x, int64_t x_stride, const void *y, int64_t y_stride, int64_t n_rows) {
+    return x == y && x_stride != y_stride && n_rows > 1;
+}
+
 int64_t norm_blocks(const tf_qk_norm_config *c, int64_t n_rows, int64_t most) {
     const int tile = norm_tile(c, n_rows);
     const int64_t tiles = (n_rows + tile - 1) / tile;
@@ -356,6 +360,9 @@ extern "C" tf_status tf_qk_norm_rotate(const tf_qk_norm_config *c, const void *q
     if (n_rows == 0) return TF_OK;
     if (!q || !k || !q_gain || !k_gain || !q_out || !k_out) return TF_EINVAL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(q_gain) || !aligned16(k_gain) || !aligned16(q_out) || !aligned16(k_out))
+        return TF_EINVAL;
+    if (in_place_elsewhere(q, q_stride, q_out, q_out_stride, n_rows) || in_place_elsewhere(k, k_stride, k_out, k_out_stride, n_rows) ||
+        over_inputs({q_out}, {k, q_gain, k_gain}) || over_inputs({k_out}, {q, q_gain, k_gain}) || q_out == k_out)
         return TF_EINVAL;
     NormArgs A = {};
     A.x[0] = q, A.x[1] = k, A.y[0] = q_out, A.y[1] = k_out, A.gain[0] = q_gain, A.gain[1] = k_gain;
@@ -386,6 +393,10 @@ extern "C" tf_status tf_qk_norm_rotate_backward(const tf_qk_norm_config *c, cons
     if (n_rows > 0) {
         if (!q || !k || !dq_out || !dk_out || !dq || !dk) return TF_EINVAL;
         if (!aligned16(q) || !aligned16(k) || !aligned16(dq_out) || !aligned16(dk_out) || !aligned16(dq) || !aligned16(dk))
+            return TF_EINVAL;
+        if (in_place_elsewhere(dq_out, dq_out_stride, dq, dq_stride, n_rows) ||
+            in_place_elsewhere(dk_out, dk_out_stride, dk, dk_stride, n_rows) || over_inputs({dq}, {dk_out, q, k, q_gain, k_gain}) ||
+            over_inputs({dk}, {dq_out, q, k, q_gain, k_gain}) || dq == dk)
             return TF_EINVAL;
     }
     NormArgs A = {};

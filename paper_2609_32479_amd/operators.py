@@ -181,6 +181,8 @@ def _offsets(offsets, like: torch.Tensor) -> int:
     _same("offsets", offsets, like, torch.int32)
     if offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous():
         raise ValueError("offsets must be a contiguous int32 vector of at least one element")
+    if offsets.numel() > 2 ** 31:
+        raise ValueError("offsets must be those of fewer than 2^31 sequences")
     return offsets.numel() - 1
 
 
