@@ -383,6 +383,9 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                     if (A.out_f32) ((float *)A.out)[r * A.os + h * DV + i] = nan;
                     else ((typename T::E *)A.out)[r * A.os + h * DV + i] = (typename T::E)nan;
                 }
+            if (A.sf)
+                for (long long s = p; s < A.n_seqs; s += A.spans.n)
+                    for (int i = tid; i < DK * DV; i += NT) A.sf[(s * A.heads + h) * (DK * DV) + i] = nan;
         }
         return;
     }
@@ -796,10 +799,12 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
 // First and past-the-last row of every row's sequence; whether the offsets are in order and inside the array.  A workgroup
 // has 1024 rows: it finds the sequence of the first by 256 probes at a time, puts the starts of the sequences that follow
 // where they are, and a running maximum tells every row its sequence (a thread a row and a binary search each took 92 us
-// for 918 161 rows of 65 536 sequences).
+// for 918 161 rows of 65 536 sequences).  The workgroups behind those pass the states of sequences without rows through,
+// `per` sequences each (a launch of their own took 4 us).
 __global__ __launch_bounds__(256) void tf_decay_index_kernel(const int32_t *__restrict__ offsets, int n_seqs, int n_rows,
                                                              int2 *__restrict__ info, int *__restrict__ bad,
-                                                             int32_t *__restrict__ flags) {
+                                                             int32_t *__restrict__ flags, long long size, int per,
+                                                             const float *__restrict__ s0, float *__restrict__ sf) {
     __shared__ int mark[kIndexRows], top[4];
     const int tid = threadIdx.x;
     if (blockIdx.x < kCheckers) {
@@ -816,7 +821,21 @@ __global__ __launch_bounds__(256) void tf_decay_index_kernel(const int32_t *__re
         }
         return;
     }
-    const int r0 = (int)(blockIdx.x - kCheckers) * kIndexRows, r1 = n_rows - r0 < kIndexRows ? n_rows : r0 + kIndexRows;
+    const int tile = (int)blockIdx.x - kCheckers, tiles = (n_rows + kIndexRows - 1) / kIndexRows;
+    if (tile >= tiles) {
+        const long long first = (long long)(tile - tiles) * per, end = first + per < n_seqs ? first + per : n_seqs;
+        for (long long s = first; s < end; s += 64) {
+            const long long mine = s + tid % 64;  // (every wave looks at all of them)
+            unsigned long long empty = __ballot(mine < end && offsets[mine < end ? mine : s] == offsets[mine < end ? mine + 1 : s]);
+            for (; empty; empty &= empty - 1) {
+                const long long i = s + __builtin_ctzll(empty);
+                for (long long e = 4 * tid; e < size; e += 1024)
+                    *(o_f32x4 *)(sf + i * size + e) = s0 ? *(const o_f32x4 *)(s0 + i * size + e) : o_f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+        }
+        return;
+    }
+    const int r0 = tile * kIndexRows, r1 = n_rows - r0 < kIndexRows ? n_rows : r0 + kIndexRows;
     // how many of the n_seqs + 1 offsets are at most r0
     int lo = 0, hi = n_seqs + 1;
     while (lo < hi) {
@@ -913,18 +932,6 @@ __global__ __launch_bounds__(256) void tf_decay_chain_kernel(DecayRuns R, int si
                 add(1, i + BATCH);
             }
         }
-    }
-}
-
-// States of sequences without rows: the first one passes through.  With bad offsets all are NaN.
-__global__ __launch_bounds__(256) void tf_decay_empty_kernel(const int32_t *__restrict__ offsets, int n_seqs, long long size,
-                                                             const float *__restrict__ s0, float *__restrict__ sf,
-                                                             const int *bad) {
-    const bool wrong = any_bad(bad);
-    for (int i = blockIdx.x; i < n_seqs; i += gridDim.x) {
-        if (!wrong && offsets[i] != offsets[i + 1]) continue;
-        for (long long e = threadIdx.x; e < size; e += 256)
-            sf[i * size + e] = wrong ? __builtin_nanf("") : s0 ? s0[i * size + e] : 0.0f;
     }
 }
 
@@ -1211,13 +1218,12 @@ void chain_run(int elem, DecayRuns R, int runs, int dk, int dv, hipStream_t s) {
     hipLaunchKernelGGL(tf_decay_chain_kernel, dim3((unsigned)(chains / 4 * A.heads), (unsigned)(dk * dv / 128), runs), dim3(256), 0, s, R,
                        dk * dv, chains);
 }
-void index_run(const int32_t *offsets, int n_seqs, int64_t n_rows, const Plan &p, int32_t *flags, hipStream_t s) {
-    hipLaunchKernelGGL(tf_decay_index_kernel, dim3((unsigned)(kCheckers + (n_rows + kIndexRows - 1) / kIndexRows)), dim3(256), 0, s, offsets, n_seqs,
-                       (int)n_rows, p.info, p.bad, flags);
-}
-void empty_run(const int32_t *offsets, int n_seqs, long long size, const float *s0, float *sf, const Plan &p, hipStream_t s) {
-    hipLaunchKernelGGL(tf_decay_empty_kernel, dim3(n_seqs < 1024 ? n_seqs : 1024), dim3(256), 0, s, offsets, n_seqs, size, s0, sf,
-                       p.bad);
+// (s0, sf: the states of `size` values that sequences without rows pass through; sf null: none)
+void index_run(const int32_t *offsets, int n_seqs, int64_t n_rows, const Plan &p, int32_t *flags, long long size, const float *s0,
+               float *sf, hipStream_t s) {
+    const int64_t per = ((int64_t)n_seqs + 1023) / 1024, states = sf && per ? (n_seqs + per - 1) / per : 0;
+    hipLaunchKernelGGL(tf_decay_index_kernel, dim3((unsigned)(kCheckers + (n_rows + kIndexRows - 1) / kIndexRows + states)), dim3(256), 0, s,
+                       offsets, n_seqs, (int)n_rows, p.info, p.bad, flags, size, (int)per, s0, sf);
 }
 template <class T>
 void share_one(const DecayShare &S, const tf_decay_config *c, int64_t n_rows, const int32_t *offsets, int n_seqs, const int *bad, hipStream_t s) {
@@ -1278,10 +1284,8 @@ extern "C" tf_status tf_decay_attention(const tf_decay_config *c, const void *q,
     if (over_inputs({out, final_state}, {initial_state})) return TF_EINVAL;
     const Plan p = decay_plan(c, n_rows, n_seqs, false, false, workspace);
     if (workspace_bytes < p.bytes) return TF_EINVAL;
-    index_run(offsets, n_seqs, n_rows, p, flags, stream);
-    if (final_state)
-        empty_run(offsets, n_seqs, (long long)c->n_heads * c->d_k * c->d_v, initial_state, final_state, p, stream);
-    if (n_rows > 0) {
+    index_run(offsets, n_seqs, n_rows, p, flags, (long long)c->n_heads * c->d_k * c->d_v, initial_state, final_state, stream);
+    if (n_rows > 0 || final_state) {
         DecayRun A = {};
         const int group = c->n_heads / c->n_qk_heads;
         A.q = q, A.k = k, A.v = v, A.qs = q_stride, A.ks = k_stride, A.vs = v_stride;
@@ -1328,14 +1332,12 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
     const Plan p = decay_plan(c, n_rows, n_seqs, true, d_state != nullptr, workspace);
     if (workspace_bytes < p.bytes) return TF_EINVAL;
     const int H = c->n_heads, group = H / c->n_qk_heads, dir = c->reverse ? -1 : 1, size = c->d_k * c->d_v;
-    const long long states = (long long)H * size;
-    index_run(offsets, n_seqs, n_rows, p, flags, stream);
-    if (n_seqs > 0 && d_initial) empty_run(offsets, n_seqs, states, d_state, d_initial, p, stream);
+    index_run(offsets, n_seqs, n_rows, p, flags, (long long)H * size, d_state, d_initial, stream);
     DecayRun A = {};
     A.group = group, A.g = log_decay, A.gs = decay_stride;
     A.offsets = offsets, A.n_seqs = n_seqs, A.heads = H, A.bad = p.bad;
     A.spans = {p.info, (int)n_rows, decay_span(c, n_rows), (int)decay_spans(c, n_rows)};
-    if (n_rows > 0 && n_seqs > 0) {
+    if (n_seqs > 0 && (n_rows > 0 || d_initial)) {
         // the states at the spans' ends, and their gradients
         DecayRun F = A;
         F.k = k, F.ks = k_stride, F.kg = 1, F.v = v, F.vs = v_stride;
@@ -1375,7 +1377,7 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
             span_run(c->elem, {{Q, K}}, 2, c->d_v, c->d_k, DECAY_DOT, stream);
             span_run(c->elem, {{V}}, 1, c->d_k, c->d_v, DECAY_OUT, stream);
         }
-        if (shared) {
+        if (shared && n_rows > 0) {
             share_run({{p.dq, p.dk}, {dq, dk}, {dq_stride, dk_stride}}, c, n_rows, offsets, n_seqs, p.bad, stream);
         }
     }

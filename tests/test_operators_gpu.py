@@ -268,6 +268,32 @@ def test_empty_batches(tf):
             assert bool((d == (0 if g.dim() == 1 else -7)).all())
 
 
+def test_states_of_many_sequences_without_rows_pass_through(tf):
+    n = 2500
+    lens = [i % 3 if i % 7 else 0 for i in range(n)]
+    t, off, rows = _attn_inputs(33, BF16, lens, 2, 1, 32, 32)
+    c, o = _cuda(t), torch.from_numpy(off).cuda()
+    s0, ds = (torch.randn(n, 2, 32, 32, device="cuda") for _ in range(2))
+    empty = torch.tensor([l == 0 for l in lens], device="cuda")
+    _, last = tf.decay_attention(c["q"], c["k"], c["v"], c["g"], o, initial_state=s0, return_state=True)
+    assert torch.equal(last[empty], s0[empty]) and not bool((last[~empty] == s0[~empty]).all(-1).any())
+    _, zero = tf.decay_attention(c["q"], c["k"], c["v"], c["g"], o, return_state=True)
+    assert bool((zero[empty] == 0).all())
+    got = tf.decay_attention_backward(c["d_out"], c["q"], c["k"], c["v"], c["g"], o, initial_state=s0, d_state=ds)
+    assert torch.equal(got[4][empty], ds[empty])
+    # no rows at all, and offsets that say otherwise: every state is NaN
+    none = c["q"][:0], c["k"][:0], c["v"][:0], c["g"][:0]
+    for bad in (False, True):
+        z = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+        z[-1] = int(bad)
+        _, last = tf.decay_attention(*none, z, initial_state=s0, return_state=True)
+        got = tf.decay_attention_backward(c["d_out"][:0], *none, z, initial_state=s0, d_state=ds)
+        if bad:
+            assert bool(last.isnan().all()) and bool(got[4].isnan().all())
+        else:
+            assert torch.equal(last, s0) and torch.equal(got[4], ds)
+
+
 def test_far_rows_of_a_large_batch(tf):
     """Element offsets past 2^31: the last sequence of a batch of 2.3 G values is that of a small call."""
     heads, d, L, n = 16, 128, 7001, 160
