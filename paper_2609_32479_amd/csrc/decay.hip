@@ -991,9 +991,9 @@ __global__ __launch_bounds__(256) void tf_decay_dots_kernel(DecayGrad A) {
 }
 
 // The decays' gradient of a span and head: sums from the span's last row (in the recurrence's order) to
-// its first, sequence by sequence.  The sums are fp64, so that rows far from the end lose nothing.
-__global__ __launch_bounds__(64) void tf_decay_grad_kernel(DecayGrad A) {
-    const int p = blockIdx.x / A.heads, h = blockIdx.x % A.heads, i = threadIdx.x, dir = -A.dir;
+// its first, sequence by sequence, by one wave (lane i).  The sums are fp64, so that rows far from the end lose nothing.
+__device__ __forceinline__ void decay_grad(const DecayGrad &A, int item, int i) {
+    const int p = item / A.heads, h = item % A.heads, dir = -A.dir;
     if (any_bad(A.bad)) {
         const float nan = __builtin_nanf("");
         const long long lo = (long long)p * A.spans.span;
@@ -1047,24 +1047,37 @@ __global__ __launch_bounds__(64) void tf_decay_sum_kernel(const float *__restric
 struct DecayShare {
     const float *part[2];  // dq, dk
     void *out[2];
-    long long stride[2];
+    long long stride[2], n_rows;
+    const int32_t *offsets;
+    const int *bad;
+    int group, shared, width, n_seqs, blocks;  // heads that share one; how many are shared; workgroups of each
 };
-template <class T>
-__global__ __launch_bounds__(256) void tf_decay_share_kernel(DecayShare S, int group, int shared, int width, long long n_rows,
-                                                             const int32_t *__restrict__ offsets, int n_seqs, const int *bad) {
-    const float *part = blockIdx.y ? S.part[1] : S.part[0];
-    typename T::E *out = (typename T::E *)(blockIdx.y ? S.out[1] : S.out[0]);
-    const long long stride = blockIdx.y ? S.stride[1] : S.stride[0];
-    const int per = shared * width / 4;
-    const bool wrong = any_bad(bad);
-    const long long lo = wrong ? 0 : offsets[0], hi = wrong ? n_rows : offsets[n_seqs];
-    for (long long i = lo * per + (long long)blockIdx.x * 256 + threadIdx.x; i < hi * per; i += (long long)gridDim.x * 256) {
+template <class T> __device__ __forceinline__ void decay_share(const DecayShare &S, int which, int block, int blocks, int tid) {
+    const float *part = S.part[which];
+    typename T::E *out = (typename T::E *)S.out[which];
+    const long long stride = S.stride[which];
+    const int per = S.shared * S.width / 4;
+    const bool wrong = any_bad(S.bad);
+    const long long lo = wrong ? 0 : S.offsets[0], hi = wrong ? S.n_rows : S.offsets[S.n_seqs];
+    for (long long i = lo * per + (long long)block * 256 + tid; i < hi * per; i += (long long)blocks * 256) {
         const long long r = i / per;
-        const int c = (int)(i - r * per) * 4, hk = c / width, d = c - hk * width;
-        const float *p = part + (r * shared + hk) * (long long)group * width + d;
+        const int c = (int)(i - r * per) * 4, hk = c / S.width, d = c - hk * S.width;
+        const float *p = part + (r * S.shared + hk) * (long long)S.group * S.width + d;
         o_f32x4 v = *(const o_f32x4 *)p;
-        for (int j = 1; j < group; ++j) v += *(const o_f32x4 *)(p + (long long)j * width);
+        for (int j = 1; j < S.group; ++j) v += *(const o_f32x4 *)(p + (long long)j * S.width);
         store4<T>(out + r * stride + c, v);
+    }
+}
+
+// Both, as they wait for different things: the decays' gradient for one row sum after another (a wave a span and head,
+// first of the launch), the sums over sharing heads for memory.  Apart they took 7 and 9 us for 9.6 thousand rows.
+template <class T> __global__ __launch_bounds__(256) void tf_decay_last_kernel(DecayGrad G, DecayShare S) {
+    const int items = G.spans.n * G.heads, waves = (items + 3) / 4, share = (int)blockIdx.x - waves;
+    if (share < 0) {
+        const int item = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        if (item < items) decay_grad(G, item, threadIdx.x % 64);
+    } else {
+        decay_share<T>(S, share & 1, share >> 1, S.blocks, threadIdx.x);
     }
 }
 
@@ -1225,16 +1238,11 @@ void index_run(const int32_t *offsets, int n_seqs, int64_t n_rows, const Plan &p
     hipLaunchKernelGGL(tf_decay_index_kernel, dim3((unsigned)(kCheckers + (n_rows + kIndexRows - 1) / kIndexRows + states)), dim3(256), 0, s,
                        offsets, n_seqs, (int)n_rows, p.info, p.bad, flags, size, (int)per, s0, sf);
 }
-template <class T>
-void share_one(const DecayShare &S, const tf_decay_config *c, int64_t n_rows, const int32_t *offsets, int n_seqs, const int *bad, hipStream_t s) {
-    const int64_t items = n_rows * c->n_qk_heads * c->d_k / 4, blocks = (items + 255) / 256;
-    hipLaunchKernelGGL((tf_decay_share_kernel<T>), dim3((unsigned)(blocks < 8192 ? blocks : 8192), 2), dim3(256), 0, s, S,
-                       c->n_heads / c->n_qk_heads, (int)c->n_qk_heads, (int)c->d_k, (long long)n_rows, offsets, n_seqs, bad);
-}
-void share_run(const DecayShare &S, const tf_decay_config *c, int64_t n_rows, const int32_t *offsets, int n_seqs, const int *bad, hipStream_t s) {
-    if (c->elem == TF_ELEM_BF16) share_one<ElemBF16>(S, c, n_rows, offsets, n_seqs, bad, s);
-    else if (c->elem == TF_ELEM_FP32) share_one<ElemF32>(S, c, n_rows, offsets, n_seqs, bad, s);
-    else share_one<ElemF16>(S, c, n_rows, offsets, n_seqs, bad, s);
+void last_run(int elem, const DecayGrad &G, const DecayShare &S, hipStream_t s) {
+    const dim3 grid((unsigned)((G.spans.n * G.heads + 3) / 4 + 2 * S.blocks)), block(256);
+    if (elem == TF_ELEM_BF16) hipLaunchKernelGGL((tf_decay_last_kernel<ElemBF16>), grid, block, 0, s, G, S);
+    else if (elem == TF_ELEM_FP32) hipLaunchKernelGGL((tf_decay_last_kernel<ElemF32>), grid, block, 0, s, G, S);
+    else hipLaunchKernelGGL((tf_decay_last_kernel<ElemF16>), grid, block, 0, s, G, S);
 }
 
 bool decay_sizes_ok(const tf_decay_config *c, int64_t n_rows, int32_t n_seqs) {
@@ -1333,6 +1341,7 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
     if (workspace_bytes < p.bytes) return TF_EINVAL;
     const int H = c->n_heads, group = H / c->n_qk_heads, dir = c->reverse ? -1 : 1, size = c->d_k * c->d_v;
     index_run(offsets, n_seqs, n_rows, p, flags, (long long)H * size, d_state, d_initial, stream);
+    DecayShare S = {};
     DecayRun A = {};
     A.group = group, A.g = log_decay, A.gs = decay_stride;
     A.offsets = offsets, A.n_seqs = n_seqs, A.heads = H, A.bad = p.bad;
@@ -1377,8 +1386,10 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
             span_run(c->elem, {{Q, K}}, 2, c->d_v, c->d_k, DECAY_DOT, stream);
             span_run(c->elem, {{V}}, 1, c->d_k, c->d_v, DECAY_OUT, stream);
         }
-        if (shared && n_rows > 0) {
-            share_run({{p.dq, p.dk}, {dq, dk}, {dq_stride, dk_stride}}, c, n_rows, offsets, n_seqs, p.bad, stream);
+        if (shared) {
+            const int64_t items = n_rows * c->n_qk_heads * c->d_k / 4, blocks = (items + 255) / 256;
+            S = {{p.dq, p.dk}, {dq, dk}, {dq_stride, dk_stride}, n_rows, offsets, p.bad, group, c->n_qk_heads, c->d_k, n_seqs,
+                 (int)(blocks < 8192 ? blocks : 8192)};
         }
     }
     DecayGrad G = {};
@@ -1391,7 +1402,7 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
             hipLaunchKernelGGL(tf_decay_dots_kernel, dim3((unsigned)((items + 3) / 4)), dim3(256), 0, stream, G);
     }
     if (n_rows > 0 || !decay_stride)
-        hipLaunchKernelGGL(tf_decay_grad_kernel, dim3((unsigned)(G.spans.n * H)), dim3(64), 0, stream, G);
+        last_run(c->elem, G, S, stream);
     if (!decay_stride)
         hipLaunchKernelGGL(tf_decay_sum_kernel, dim3(H), dim3(64), 0, stream, p.part, G.spans.n, H, d_log_decay);
     return hipGetLastError() == hipSuccess ? TF_OK : TF_EHIP;
