@@ -338,10 +338,18 @@ constexpr int tile_list(int a, int b, int c, int d, int e, int f, int g, int h, 
 constexpr int kTileT = tile_list(3, 2, 1, 3, 0, 3, 2, 2, 1, 3), kTileS = tile_list(3, 2, 1, 0, 0, 2, 1, 0, 0, 1);
 __device__ __forceinline__ int tile_of(int list, int w) { return list >> (2 * w) & 3; }
 
-// One span of one head, four waves.  A wave owns a quarter of the state's and the output's columns (d_v 32: half, and
-// of the outputs every second row tile; its pair holds the same state); the state stays in its accumulators over the span.  The 64 x 64 weights of a chunk are computed once,
-// 16 x 16 tiles on or below the diagonal dealt out to the waves, and pass through LDS; the last
-// wave prepares the next chunk's row sums meanwhile.  The next chunk's rows of the tensors are on their way to registers.
+// One span of one head.  A wave (four of them, eight for d_v 128) owns 16 of the state's and the output's columns (d_v 32: 16
+// of them too, and of the outputs every second row tile; its pair holds the same state); the state stays in its accumulators
+// over the span.  The 64 x 64 weights of a chunk are computed once, 16 x 16 tiles on or below the diagonal dealt out to the
+// waves, and pass through LDS; the last wave prepares the next chunk's row sums meanwhile.  The next chunk's rows of the
+// tensors are on their way to registers.
+//
+// Chunks of 64 rows: a chunk's weights cost 64 (d_k + d_v) products a row and its state 2 d_k d_v, equal at 64 columns, and
+// tracks of up to 20 hits are whole within one or two.  What bounds it: with many spans, memory.  918 161 rows of 65 536 tracks,
+// 3 heads of 64 x 64, bf16: 1.42 GB in 342 us, 4.2 TB/s of the 5.1 that a copy reaches, the vector units 42 % busy.  With few,
+// the latency of a chunk's phases, each behind a barrier (about 7 us a chunk at 2 GHz): one sequence of 32 768 rows, 8 heads of
+// 128 x 128, 512 workgroups: states 44 us, outputs 98 us, the matrix units a fifth and the vector units a third busy.
+// fp32: the fp32 instruction (16 times slower than bf16's) and LDS: gradients of 115 thousand rows, 4 heads of 32 x 32, 277 us.
 template <class T, int DK, int DV, int MODE>
 __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ? 4 : 3) : DK * DV <= 32 * 32 || MODE == DECAY_OUT && DK * DV <= 64 * 64 ? 3 : 2) void tf_decay_span_kernel(DecayRuns R) {
     typedef typename MatOf<T>::M M;
@@ -523,11 +531,9 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         const int at = chunk_at(c), rows = chunk_rows(at);
         const ChunkRows &W = rows_of[c & 1];
         const bool slow = __builtin_amdgcn_readfirstlane(wild[c & 1]);
-        // (behind the last chunk there is nothing to fetch; a large state's kernel is better off without the branch, loading
-        // that chunk again: tracks' gradients at 32 columns, fp32, 301 us with the branch and 318 without, long sequences'
-        // outputs at 128 columns, bf16, 174 us with it and 167 without)
-        if (DK * DV > 64 * 64) fetch(c + 1 < chunks ? c + 1 : c);
-        else if (c + 1 < chunks) fetch(c + 1);
+        // (Behind the last chunk that chunk again: under a branch the loads are waited for where it ends.  One sequence of 32 768
+        // rows, 8 heads of 128 x 128: 171 us with a branch, 157 without; tracks' gradients in fp32 301 and 300.)
+        fetch(c + 1 < chunks ? c + 1 : c);
         F vf[NB][CT];  // the wave's columns of v, for the state and for the output
         auto read_v = [&](int k) {
 #pragma unroll
@@ -878,7 +884,8 @@ __global__ __launch_bounds__(256) void tf_decay_index_kernel(const int32_t *__re
 
 // The states at the spans' ends from the spans' own contributions, in order along each cut sequence.  A wave has 128
 // values of one head's states and every `chains`-th span; where that is a sequence's first cut it follows the sequence, the
-// next spans' contributions on their way while it adds (each sum stays for the span that follows).
+// next spans' contributions on their way while it adds (each sum stays for the span that follows).  A chain's latency bounds
+// it: 64 spans of 8 heads of 128 x 128, 67 MB read and written in 13 us.
 __global__ __launch_bounds__(256) void tf_decay_chain_kernel(DecayRuns R, int size, int chains) {
     const DecayRun &A = R.run[blockIdx.z];
     if (any_bad(A.bad)) return;
@@ -1083,7 +1090,8 @@ template <class T> __global__ __launch_bounds__(256) void tf_decay_last_kernel(D
 
 // One token of every sequence: the state is read, decayed, added to, multiplied with q and written in one
 // pass.  A workgroup of 256 threads has one head's state; a thread four neighbouring columns of every
-// 256 / (dv / 4)-th row.
+// 256 / (dv / 4)-th row.  Memory bounds it: 509 sequences of 16 heads of 64 x 128, 538 MB in 98 us (5.5 TB/s; a copy reaches
+// 5.1).
 template <class T>
 __global__ __launch_bounds__(256) void tf_decay_step_kernel(const void *__restrict__ q_, long long qs, const void *__restrict__ k_,
                                                             long long ks, const void *__restrict__ v_, long long vs,
@@ -1134,9 +1142,9 @@ tf_status decay_check(const tf_decay_config *c) {
 }
 
 // Rows of a span.  Enough spans that the compute units have four workgroups each (two of the wide heads', which hold
-// fewer), and no more than that: every border that cuts a sequence costs a state written and read.  32 768 rows of 8 heads of
-// 128 x 128, the three launches: spans of 128 366 us, 256 281, 512 234, 1024 303.  Not beyond 512 rows: the last workgroups'
-// share of 918 161 rows of tracks grows (spans of 512 407 us, 1024 413, 2048 437).
+// fewer), and no more than that: every border that cuts a sequence costs a state written and read.  One sequence of 32 768 rows,
+// 8 heads of 128 x 128: spans of 128 rows 239 us, 256 194, 512 157, 1024 154.  Not beyond 512 rows: the last workgroups' share of
+// 918 161 rows of tracks grows (spans of 512 362 us, 1024 367, 2048 373).
 int decay_span(const tf_decay_config *c, int64_t n_rows) {
     int64_t s = n_rows * c->n_heads / (c->d_k * c->d_v > 64 * 64 ? 512 : 1024) / kChunk * kChunk;
     if (s < kMinSpan) s = kMinSpan;
@@ -1379,7 +1387,7 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
         V.q = k, V.qs = k_stride, V.qg = 1;
         V.out = dv, V.os = dv_stride;
         V.sf = d_initial, V.sf_decay = 1;
-        if (c->d_k == c->d_v) {  // (apart they took 63 and 27 us for 9.6 thousand rows, which leave compute units idle)
+        if (c->d_k == c->d_v) {  // (9.6 thousand rows, which leave compute units idle: together 73 us, apart 59 and 27)
             V.x = nullptr;
             span_run(c->elem, {{Q, K, V}}, 3, c->d_k, c->d_v, DECAY_DOT, stream);
         } else {
