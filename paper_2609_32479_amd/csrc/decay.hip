@@ -532,7 +532,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         const ChunkRows &W = rows_of[c & 1];
         const bool slow = __builtin_amdgcn_readfirstlane(wild[c & 1]);
         // (Behind the last chunk that chunk again: under a branch the loads are waited for where it ends.  One sequence of 32 768
-        // rows, 8 heads of 128 x 128: 171 us with a branch, 157 without; tracks' gradients in fp32 301 and 300.)
+        // rows, 8 heads of 128 x 128: 171 us with a branch, 157 without; 65 536 tracks 360 and 342.)
         fetch(c + 1 < chunks ? c + 1 : c);
         F vf[NB][CT];  // the wave's columns of v, for the state and for the output
         auto read_v = [&](int k) {

@@ -19,7 +19,7 @@
 // Everything between the loads and the one rounding at the store is fp32.
 //
 // Memory bounds it: 918 thousand rows of 3 + 3 heads of 64, bf16, 1.41 GB in 310 us (4.5 TB/s; a copy reaches 5.1), and
-// backward 18 thousand rows of 16 + 4 heads of 128, 342 MB in 90 us (3.8 TB/s), 7 of them the gains' sums, whose launch is
+// backward 22 thousand rows of 16 + 4 heads of 128, 342 MB in 90 us (3.8 TB/s), 7 of them the gains' sums, whose launch is
 // latency.  16 values a lane: a lane then has both halves of its pairs in two or four 16-byte loads, and a head's sums are two
 // to four exchanges; 32 registers of gains' sums still leave the backward pass its four workgroups a compute unit.
 #include "ops.h"
