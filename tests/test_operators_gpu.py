@@ -294,6 +294,35 @@ def test_states_of_many_sequences_without_rows_pass_through(tf):
             assert torch.equal(last, s0) and torch.equal(got[4], ds)
 
 
+def _spread(x, stride):
+    """The same rows, `stride` elements apart."""
+    y = torch.empty(x.shape[0] * stride, dtype=x.dtype, device=x.device).view(x.shape[0], stride)[:, :x[0].numel()].unflatten(1, x.shape[1:])
+    y.copy_(x)
+    return y
+
+
+def test_rows_as_far_apart_as_strides_go(tf):
+    """Offsets inside a tile up to 2^32 bytes: the results are those of contiguous rows, bit for bit."""
+    t, off, rows = _attn_inputs(41, torch.float32, [3, 66, 1], 2, 1, 32, 32)
+    c, o = _cuda(t), torch.from_numpy(off).cuda()
+    far = {x: _spread(c[x], 1 << 24) for x in ("q", "k", "v", "d_out")}
+    want, last = tf.decay_attention(c["q"], c["k"], c["v"], c["g"], o, return_state=True)
+    got, last2 = tf.decay_attention(far["q"], far["k"], far["v"], c["g"], o, return_state=True)
+    assert torch.equal(want, got) and torch.equal(last, last2)
+    for x, y in zip(tf.decay_attention_backward(c["d_out"], c["q"], c["k"], c["v"], c["g"], o)[:4],
+                    tf.decay_attention_backward(far["d_out"], far["q"], far["k"], far["v"], c["g"], o)[:4]):
+        assert torch.equal(x, y)
+    del far
+    x, gain = torch.randn(300, 2, 32, device="cuda"), torch.ones(32, device="cuda")
+    far = _spread(x, 1 << 22)
+    assert all(torch.equal(a, b) for a, b in zip(tf.qk_norm_rotate(x, x.clone(), gain, gain), tf.qk_norm_rotate(far, x, gain, gain)))
+    x, d = torch.randn(300, 40, device="cuda"), torch.randn(300, 50, device="cuda")
+    w, u = torch.randn(50, 40, device="cuda"), torch.randn(50, 40, device="cuda")
+    far = _spread(x, 1 << 22)
+    assert torch.equal(tf.gated_ffn(x, w, u), tf.gated_ffn(far, w, u))
+    assert all(torch.equal(a, b) for a, b in zip(tf.gated_ffn_backward(d, x, w, u), tf.gated_ffn_backward(d, far, w, u)))
+
+
 def test_far_rows_of_a_large_batch(tf):
     """Element offsets past 2^31: the last sequence of a batch of 2.3 G values is that of a small call."""
     heads, d, L, n = 16, 128, 7001, 160
