@@ -183,7 +183,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tf_gated_kernel(GatedArgs A) 
         }
     };
     const long long n0 = (long long)tn * BN;
-    const int f0 = tn * (BN / 2);
+    const int f0 = tn * (BN / 2) < A.F ? tn * (BN / 2) : A.F - 1;  // (the padding's tiles read the last inner value)
 #pragma unroll
     for (int i = 0; i < LM; ++i) {
         const int piece = i * NT + tid;
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tf_gated_kernel(GatedArgs A) 
             for (int i = 0; i < LM; ++i) dma16(m, mo[i], to + i * NT * 16);
 #pragma unroll
             for (int i = 0; i < LN; ++i) {
-                // (which weight a piece is of is the same for the whole wave: 8 rows of 32 or 64)
+                // (which weight a piece is of is the same for the whole wave: 8 rows of 16, 32 or 64)
                 const bool up = NA && __builtin_amdgcn_readfirstlane((i * NT + tid) / 8 % (BN / WN)) >= BN / WN / 2;
                 dma16(up ? n2 : n, no[i], to + BM * 128 + i * NT * 16);
             }
@@ -482,11 +482,15 @@ bool gated_fits(const tf_gated_config *c, int64_t n_rows, std::initializer_list<
 int64_t gated_pad(const tf_gated_config *c) { return ((int64_t)c->inner + 63) / 64 * 64; }
 
 // The tiles of a product of m x n: 256 x 256, one workgroup of eight waves a compute unit, or 128 x 128, two of four waves,
-// each with a ring of two stages.  Whole rounds of the compute units' tiles are paid for; a round of pairs of small tiles
+// each with a ring of two stages (and 64 x 64 for few tiles, below).  Whole rounds of the compute units' tiles are paid for; a round of pairs of small tiles
 // takes 0.62 of one of large ones, for half its products.  5003 x 1032 with sums of 5504: 77 us in small tiles, 126 in
 // large ones; 256 x 128 with three stages and 128 x 128 with four, one workgroup a compute unit: 88 and 124.
-constexpr int kShapes[2] = {256, 128};
+constexpr int kShapes[3] = {256, 128, 64};
 constexpr double kRound[2] = {1.0, 0.62};
+// Tiles of 128 x 128 up to which the projections, whose sums are not split, take 64 x 64 (up to five workgroups a compute unit):
+// 1024 -> 2 x 4096, bf16, 128 rows (64 tiles) 7.8 us for 12.6, 300 rows (192) 12.0 for 13.5, 400 rows (256) 14.6 for 14.1; fp32,
+// whose products take sixteen times as long, 128 rows 26 us for 72, 600 (320) 98 for 123, 800 (448) 119 for 124.
+template <class T> constexpr int64_t kFewTiles = sizeof(typename T::E) == 4 ? 512 : 192;
 int64_t gated_tiles(int64_t m, int64_t n, int shape) {
     const int b = kShapes[shape];
     return ((m + b - 1) / b) * ((n + b - 1) / b);
@@ -539,7 +543,14 @@ template <class T, int ROLE, bool GELU> void gated_product(const GatedArgs &A, i
             return;
         }
     }
-    if (gated_shape(A.M, ROLE == GATED_H || ROLE == GATED_D ? 2 * A.N : A.N) == 0) gated_tile<T, ROLE, 0, GELU, false>(A, 1, s);
+    const int64_t n = ROLE == GATED_H || ROLE == GATED_D ? 2 * A.N : A.N;
+    if constexpr (ROLE == GATED_H || ROLE == GATED_D) {
+        if (gated_tiles(A.M, n, 1) <= kFewTiles<T>) {
+            gated_tile<T, ROLE, 2, GELU, false>(A, 1, s);
+            return;
+        }
+    }
+    if (gated_shape(A.M, n) == 0) gated_tile<T, ROLE, 0, GELU, false>(A, 1, s);
     else gated_tile<T, ROLE, 1, GELU, false>(A, 1, s);
 }
 template <class T, bool BACK, bool GELU> void gated_project(const GatedArgs &A, hipStream_t s) {

@@ -444,6 +444,13 @@ def test_gated_ffn_large_tiles_and_split_sums(tf, dtype, act, rows, width, inner
     _gated(tf, dtype, act, rows, width, inner)
 
 
+@pytest.mark.parametrize("dtype,act,rows,width,inner", [
+    (BF16, "gelu", 70, 40, 70), (FP32, "silu", 129, 72, 33), (FP16, "gelu", 65, 128, 1), (BF16, "silu", 300, 64, 100),
+    (FP32, "gelu", 600, 136, 1000), (BF16, "silu", 1700, 136, 1000), (FP32, "silu", 6500, 64, 1300)])
+def test_gated_ffn_small_and_middle_tiles(tf, dtype, act, rows, width, inner):
+    _gated(tf, dtype, act, rows, width, inner)
+
+
 def _gated(tf, dtype, act, rows, width, inner):
     print(f"[ffn] {dtype} {act} {rows} {width} {inner}", flush=True)
     gen = torch.Generator().manual_seed(rows + width)
