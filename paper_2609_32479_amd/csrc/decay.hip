@@ -21,7 +21,9 @@
 //
 // (in that direction a row's decay is its predecessor's: `shift`), and with
 // db_t = q_t dq_t - k_t dk_t the gradient of g_t is the sum of db over the
-// sequence's rows from t on, plus <dS_last, S_last>.
+// sequence's rows from t on, plus <dS_last, S_last>.  What both terms of db have
+// of the same pair of rows, or of the same row and dS_last, is one number, taken
+// away in fp64, so that a head that forgets at once keeps its digits.
 //
 // How the rows are split.  Sequences may be a handful of rows or tens of
 // thousands, and the host does not know their lengths.  So the packed rows are cut
@@ -177,10 +179,11 @@ struct DecayRun {
     float *sf;
     int turned;                          // states in memory are the transposed of this run's
     int sf_decay;                        // the last state is multiplied by the last row's own decay
+    int sf_before;                       // the state kept is that from before the last chunk, decayed to the last row
     float *local;                        // [spans][heads][state]: the state at the spans' ends
     float *mult;                         // [spans][heads]: decay over a span that is all one sequence's
     int *kind;                           // [spans]: 0 its end cuts no sequence, 1 it does, 2 and its start cuts the same
-    float *db;                           // [n_rows][heads]
+    double *db;                          // [n_rows][heads]
     int pairs;                           // db has the chunks' pairs of rows too
     float out_scale, kv_scale;
     const int32_t *offsets;
@@ -277,20 +280,33 @@ __device__ __forceinline__ double lane_of(double v, int lane) {
     const unsigned lo = __builtin_amdgcn_readlane((int)b, lane), hi = __builtin_amdgcn_readlane((int)(b >> 32), lane);
     return __builtin_bit_cast(double, (long long)((unsigned long long)hi << 32 | lo));
 }
-// The sum over the 16 lanes of a row, in all of them: neighbours, pairs, quads, halves.
-__device__ __forceinline__ float sum16(float v) {
-    v += dpp<0xb1>(v);   // quad_perm 1 0 3 2
-    v += dpp<0x4e>(v);   // quad_perm 2 3 0 1
-    v += dpp<0x141>(v);  // row_half_mirror
-    v += dpp<0x140>(v);  // row_mirror
-    return v;
-}
 // The sum over the four lanes n, n + 16, n + 32, n + 48, in all of them: halves, then rows of 16, swapped.
 __device__ __forceinline__ float sum_rows(float v) {
     const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
     const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+// Four fp64 values summed over the 16 lanes of a row: lane n has the sum of value 2 (n & 1) + (n >> 1 & 1).  Neighbours, then
+// pairs, each keep one half of the values that they add; quads and halves, rotated, are added whole.
+__device__ __forceinline__ double sum16_of_4(const double (&v)[4], int n) {
+    const bool odd = n & 1, high = n & 2;
+    const double a = (odd ? v[2] : v[0]) + dpp<0xb1>(odd ? v[0] : v[2]);  // quad_perm 1 0 3 2
+    const double b = (odd ? v[3] : v[1]) + dpp<0xb1>(odd ? v[1] : v[3]);
+    double s = (high ? b : a) + dpp<0x4e>(high ? a : b);  // quad_perm 2 3 0 1
+    s += dpp<0x128>(s);  // row_ror 8
+    return s + dpp<0x124>(s);
+}
+// The sum over the four lanes n, n + 16, n + 32, n + 48 of an fp64 value.
+__device__ __forceinline__ double sum_rows(double v) {
+    auto pair = [](unsigned lo, unsigned hi) { return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo); };
+    auto words = [&] { return __builtin_bit_cast(unsigned long long, v); };
+    const auto al = __builtin_amdgcn_permlane32_swap((unsigned)words(), (unsigned)words(), false, false);
+    const auto ah = __builtin_amdgcn_permlane32_swap((unsigned)(words() >> 32), (unsigned)(words() >> 32), false, false);
+    v = pair(al[0], ah[0]) + pair(al[1], ah[1]);
+    const auto bl = __builtin_amdgcn_permlane16_swap((unsigned)words(), (unsigned)words(), false, false);
+    const auto bh = __builtin_amdgcn_permlane16_swap((unsigned)(words() >> 32), (unsigned)(words() >> 32), false, false);
+    return pair(bl[0], bh[0]) + pair(bl[1], bh[1]);
 }
 // v summed over the lanes from `from` (this lane's own, at most this lane) to this one.
 __device__ __forceinline__ double sum_from(double v, int from, int lane) {
@@ -321,9 +337,8 @@ __device__ __forceinline__ float exp2_of(double x) {
 // What the products need to know of a chunk's rows, in the recurrence's order.
 struct ChunkRows {
     float bh[kChunk], bl[kChunk];  // sum of the log2 decays from the chunk's first row, or the sequence's, to the row: high and low part
-    float in[kChunk];              // 2^b times out_scale: what the state before brings to the row
     float to[kChunk];              // 2^(b_end - b) times kv_scale: what the row brings to the state after
-    float decay[kChunk];           // 2^b
+    float decay[kChunk];           // 2^b (times out_scale: what the state before brings to the row)
     int seg[kChunk];               // the sequence: its first row in the chunk + 1 (0: before the chunk), its last + 1 << 8, 1 << 16 if it ends there
 };
 __device__ __forceinline__ int seg_first(int s) { return (s & 255) - 1; }
@@ -337,6 +352,7 @@ constexpr int tile_list(int a, int b, int c, int d, int e, int f, int g, int h, 
 }
 constexpr int kTileT = tile_list(3, 2, 1, 3, 0, 3, 2, 2, 1, 3), kTileS = tile_list(3, 2, 1, 0, 0, 2, 1, 0, 0, 1);
 __device__ __forceinline__ int tile_of(int list, int w) { return list >> (2 * w) & 3; }
+__device__ __forceinline__ int tile_at(int mt, int ms) { return mt * (mt + 1) / 2 + ms; }  // row by row
 
 // One span of one head.  A wave (four of them, eight for d_v 128) owns 16 of the state's and the output's columns (d_v 32: 16
 // of them too, and of the outputs every second row tile; its pair holds the same state); the state stays in its accumulators
@@ -349,7 +365,7 @@ __device__ __forceinline__ int tile_of(int list, int w) { return list >> (2 * w)
 // 3 heads of 64 x 64, bf16: 1.42 GB in 342 us, 4.2 TB/s of the 5.1 that a copy reaches, the vector units 42 % busy.  With few,
 // the latency of a chunk's phases, each behind a barrier (about 7 us a chunk at 2 GHz): one sequence of 32 768 rows, 8 heads of
 // 128 x 128, 512 workgroups: states 44 us, outputs 98 us, the matrix units a fifth and the vector units a third busy.
-// fp32: the fp32 instruction (16 times slower than bf16's) and LDS: gradients of 115 thousand rows, 4 heads of 32 x 32, 277 us.
+// fp32: the fp32 instruction (16 times slower than bf16's) and LDS: gradients of 115 thousand rows, 4 heads of 32 x 32, 285 us.
 template <class T, int DK, int DV, int MODE>
 __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ? 4 : 3) : DK * DV <= 32 * 32 || MODE == DECAY_OUT && DK * DV <= 64 * 64 ? 3 : 2) void tf_decay_span_kernel(DecayRuns R) {
     typedef typename MatOf<T>::M M;
@@ -371,7 +387,8 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         Xs[DOT ? kChunk * LV : 8], Ps[OUT ? PSIZE : 8];
     __shared__ ChunkRows rows_of[2];
     __shared__ int wild[2];
-    __shared__ float rowp[DOT ? 4 : 1][kChunk], colp[DOT ? 4 : 1][kChunk], dots[DOT ? NW / RG : 1][kChunk];
+    __shared__ double rowp[DOT ? 10 : 1][16], colp[DOT ? 10 : 1][16];  // of the weights' tiles, by tile_at
+    __shared__ float dots[DOT ? NW / RG : 1][kChunk];
 
     const DecayRun &A = R.run[blockIdx.y];
     const bool dot = DOT && A.x, pairs = DOT && A.pairs;
@@ -500,7 +517,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         const double be = __shfl(b, e & 63);
         const float bf = (float)b, de = exp2_of(b);
         W.bh[i] = bf, W.bl[i] = (float)(b - (double)bf);
-        W.decay[i] = de, W.in[i] = A.out_scale * de, W.to[i] = A.kv_scale * exp2_of(be - b);
+        W.decay[i] = de, W.to[i] = A.kv_scale * exp2_of(be - b);
         W.seg[i] = (f < 0 ? 0 : f + 1) | (i < rows ? e + 1 : i + 1) << 8 | (l <= rows - 1 ? 1 << 16 : 0);
         if (!OUT) total += lane_of(b, rows - 1);
     };
@@ -578,18 +595,21 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                 }
                 *(V4 *)(Ps + p_at(mt) + n * p_ld(mt) + s) = __builtin_convertvector(a, V4);
                 if (pairs) {
-                    // products of dq's weights with q k: their sums by t and by s are what q dq and k dk have of them
-                    float row = 0.0f;
+                    // products of dq's weights with q k: their sums by t and by s are what q dq and k dk have of them.  In fp64: the
+                    // decays' gradient is a sum of these over a span, in which all pairs but the few around a row cancel
+                    double row = 0.0, four = 0.0;
+                    if (!apart) {
+                        double col[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        z[i] = s + i <= t && s + i >= f ? a[i] * z[i] : 0.0f;
-                        row += z[i];
+                        for (int i = 0; i < 4; ++i) {
+                            col[i] = s + i <= t && s + i >= f ? (double)(a[i] * z[i]) : 0.0;
+                            row += col[i];
+                        }
+                        row = sum_rows(row);
+                        four = sum16_of_4(col, n);
                     }
-                    row = sum_rows(row);
-                    if (q == 0) rowp[ms][t] = row;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) z[i] = sum16(z[i]);
-                    if (n == 0) *(o_f32x4 *)&colp[mt][s] = z;
+                    if (q == 0) rowp[tile_at(mt, ms)][n] = row;
+                    if (n < 4) colp[tile_at(mt, ms)][4 * q + 2 * (n & 1) + (n >> 1)] = four;
                 }
             }
             __syncthreads();
@@ -643,7 +663,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
 #pragma unroll
                 for (int m = 0; m < TM; ++m) {
                     const int t = 16 * row_tile(m) + n;
-                    const float f = W.in[t];
+                    const float f = A.out_scale * W.decay[t];
                     const bool on = t >= a && t < b;
 #pragma unroll
                     for (int j = 0; j < CT; ++j)
@@ -661,7 +681,8 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                 } else {
                     clear_state();
                 }
-                if (!slow) {
+                if (ends && A.sf_before) {  // (the sequence needs no state any more)
+                } else if (!slow) {
 #pragma unroll
                     for (int k = 0; k < NB; ++k) {
                         if (k * KM + KM <= a || k * KM >= b) continue;
@@ -784,12 +805,12 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         if (dot && wave == 0) {
             const int t = lane;
             if (t < rows) {
-                float z = 0.0f;
-                for (int w = 0; w < NW / RG; ++w) z += dots[w][t];
+                double z = 0.0;
+                for (int w = 0; w < NW / RG; ++w) z += (double)dots[w][t];
                 if (pairs)
                     for (int m = 0; m < 4; ++m) {
-                        if (m <= t / 16) z += rowp[m][t];
-                        if (m >= t / 16) z -= colp[m][t];
+                        if (m <= t / 16) z += rowp[tile_at(t / 16, m)][t % 16];
+                        if (m >= t / 16) z -= colp[tile_at(m, t / 16)][t % 16];
                     }
                 A.db[(long long)(lo + at + (dir > 0 ? t : rows - 1 - t)) * A.heads + h] = z;
             }
@@ -951,11 +972,11 @@ __device__ __forceinline__ float wave_sum(float v) {
 struct DecayGrad {
     Spans spans;
     const float *S, *U;          // the states and their gradients at the spans' ends
-    const float *Sl, *Ul;        // of the sequences' last rows, or null
+    const float *Sl, *Ul;        // from before the sequences' last chunks, decayed to their ends, and the last states' gradients; or null
     float *cut, *last;           // their inner products: [spans][heads], [n_seqs][heads]
     const float *g;
     long long gs;
-    const float *da, *db;        // q dq - (k dk within chunks), k dk from the states
+    const double *da, *db;       // q dq - (k dk within chunks), k dk from the states
     float *dg, *part;            // part: [spans][heads], with one decay a head
     const int32_t *offsets;
     int n_seqs, heads, dir, size;
@@ -998,7 +1019,8 @@ __global__ __launch_bounds__(256) void tf_decay_dots_kernel(DecayGrad A) {
 }
 
 // The decays' gradient of a span and head: sums from the span's last row (in the recurrence's order) to
-// its first, sequence by sequence, by one wave (lane i).  The sums are fp64, so that rows far from the end lose nothing.
+// its first, sequence by sequence, by one wave (lane i).  Both terms' pairs within a chunk are the same numbers, added in fp64,
+// so that those of rows that a head has forgotten cancel; what crosses the chunks' borders is good to fp32's digits of itself.
 __device__ __forceinline__ void decay_grad(const DecayGrad &A, int item, int i) {
     const int p = item / A.heads, h = item % A.heads, dir = -A.dir;
     if (any_bad(A.bad)) {
@@ -1011,23 +1033,33 @@ __device__ __forceinline__ void decay_grad(const DecayGrad &A, int item, int i) 
         return;
     }
     const Spans::Border b0 = A.spans.border(p), b1 = A.spans.border(p + 1);
-    const int len = b1.row - b0.row, row_first = dir > 0 ? b0.row : b1.row - 1;
+    const int olo = A.offsets[0], ohi = A.offsets[A.n_seqs];
+    const int lo = b0.row > olo ? b0.row : olo, hi = b1.row < ohi ? b1.row : ohi, len = hi - lo;
+    const int chunks = len > 0 ? (len + kChunk - 1) / kChunk : 0;  // the span kernel's
     double carry = 0.0, sum = 0.0;
     if (dir > 0 ? b0.cuts : b1.cuts) carry = (double)A.cut[(long long)(dir > 0 ? p : p + 1) * A.heads + h];
-    for (int c = 0; c < len; c += 64) {
-        const int row0 = row_first + dir * c, r = row0 + dir * i;
-        const int2 s = c + i < len ? A.spans.info[r] : int2{-1, -1};
-        const bool live = s.x >= 0;
-        int f = i;
-        double v = 0.0;
+    for (int c = 0; c < chunks; ++c) {
+        const int at = (dir > 0 ? c : chunks - 1 - c) * kChunk, rows = len - at < kChunk ? len - at : kChunk;
+        const int row0 = dir > 0 ? lo + at : lo + at + rows - 1, r = row0 + dir * i;
+        const bool live = i < rows;
+        int f = i, e = i;  // the lanes of the sequence's last row (in the recurrence's order) and of its first, in the chunk
+        double a = 0.0, b = 0.0, last = 0.0;
         if (live) {
-            f = dir > 0 ? s.x - row0 : row0 - (s.y - 1);
-            v = (double)A.da[(long long)r * A.heads + h] - (double)A.db[(long long)r * A.heads + h];
-            if (f == i && A.last) v += (double)A.last[(long long)seq_of_row(A.offsets, A.n_seqs, r) * A.heads + h];
+            const int2 s = A.spans.info[r];
+            f = dir > 0 ? s.x - row0 : row0 - (s.y - 1), e = dir > 0 ? s.y - 1 - row0 : row0 - s.x;
+            a = A.da[(long long)r * A.heads + h], b = A.db[(long long)r * A.heads + h];
+            if (f >= 0 && A.last) last = (double)A.last[(long long)seq_of_row(A.offsets, A.n_seqs, r) * A.heads + h];
         }
-        v = sum_from(v, f > 0 ? f : 0, i);
+        double v = sum_from(a - b, f > 0 ? f : 0, i);
+        if (A.last) {
+            // What crosses the end: of a sequence that ends here, what its rows in the chunk have of the last state's gradient (the
+            // same numbers that b takes away again, row by row) and what the state before them has.
+            b = sum_from(b, f > 0 ? f : 0, i);
+            const double all = __shfl(b, e < rows - 1 ? e : rows - 1) + last;
+            if (f >= 0) v += all;
+        }
         if (f < 0) v += carry;
-        carry = lane_of(v, 63);  // (the rows of a chunk before the last are 64)
+        carry = lane_of(v, rows - 1);
         if (live) {
             const float g = A.gs ? A.g[(long long)r * A.gs + h] : A.g[h];
             if (g < -104.0f) v = 0.0;  // exp(g) is 0, and so is what it is multiplied with
@@ -1171,7 +1203,8 @@ struct Plan {
     int2 *info;
     int *bad, *kind[2];
     float *local[2], *mult[2];
-    float *da, *db, *cut, *last, *sl, *part, *dq, *dk;
+    double *da, *db;
+    float *cut, *last, *sl, *part, *dq, *dk;
     size_t bytes;
 };
 Plan decay_plan(const tf_decay_config *c, int64_t n_rows, int64_t n_seqs, bool back, bool states, void *base) {
@@ -1186,8 +1219,8 @@ Plan decay_plan(const tf_decay_config *c, int64_t n_rows, int64_t n_seqs, bool b
         p.local[i] = r.take<float>(spans > 1 ? spans * h * size : 0);
     }
     if (back) {
-        p.da = r.take<float>(n_rows * h);
-        p.db = r.take<float>(n_rows * h);
+        p.da = r.take<double>(n_rows * h);
+        p.db = r.take<double>(n_rows * h);
         p.cut = r.take<float>(spans * h);
         p.part = r.take<float>(spans * h);
         if (states) {
@@ -1373,7 +1406,7 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
         Q.v = k, Q.vs = k_stride, Q.vg = 1;
         Q.x = q, Q.xs = q_stride, Q.xg = 1;
         Q.out = shared ? (void *)p.dq : dq, Q.os = shared ? (int64_t)H * c->d_k : dq_stride, Q.out_f32 = shared;
-        Q.turned = 1, Q.sf = p.sl, Q.db = p.da, Q.pairs = 1, Q.out_scale = c->scale, Q.kv_scale = 1.0f;
+        Q.turned = 1, Q.sf = p.sl, Q.sf_before = 1, Q.db = p.da, Q.pairs = 1, Q.out_scale = c->scale, Q.kv_scale = 1.0f;
         // dk
         DecayRun K = B;
         K.q = v, K.qs = v_stride, K.qg = 0;

@@ -139,3 +139,65 @@ def activation(a, kind):
         return a * s, s * (1 + a * (1 - s))
     p = 0.5 * torch.erfc(-a / math.sqrt(2.0))
     return a * p, p + a * torch.exp(-a * a / 2) / math.sqrt(2 * math.pi)
+
+
+def recurrence(q, k, v, g, offsets, scale, reverse=False, s0=None, d_out=None, d_state=None, drop=()):
+    """decay_attention and, if d_out is given, its gradients, row by row as the recurrence defines them (float64), for
+    sequences of any length.  A row's decay's gradient is e^g <gradient of the state after the row, state before it>.
+
+    q, k [R, Hk, dk], v [R, H, dv], g [R, H].  Returns a dict of "out" (zeros outside of all sequences), "state" and, with
+    d_out, "dq", "dk", "dv", "dg", "d_initial".  drop: rows at whose border with the row before the state and its gradient
+    are lost, a mistake for the tests to find."""
+    rows, hk, dk = q.shape
+    h, dv = v.shape[1], v.shape[2]
+    n, group = len(offsets) - 1, h // hk
+    Q, K = q.repeat_interleave(group, 1), k.repeat_interleave(group, 1)
+    r = {"out": torch.zeros_like(v), "state": torch.zeros(n, h, dk, dv).double()}
+    if d_out is not None:
+        r |= {"dq": torch.zeros_like(Q), "dk": torch.zeros_like(K), "dv": torch.zeros_like(v), "dg": torch.zeros_like(g),
+              "d_initial": torch.zeros_like(r["state"])}
+    e = torch.exp(g)[:, :, None, None]
+    for i in range(n):
+        order = list(range(offsets[i], offsets[i + 1]))
+        if reverse:
+            order.reverse()
+        state = torch.zeros(h, dk, dv).double() if s0 is None else s0[i].clone()
+        before = []
+        for t in order:
+            if (t + 1 if reverse else t) in drop:
+                state = torch.zeros_like(state)
+            if d_out is not None:
+                before.append(state)
+            state = e[t] * state + K[t][:, :, None] * v[t][:, None, :]
+            r["out"][t] = scale * (Q[t][:, None, :] @ state)[:, 0]
+            if d_out is not None:
+                r["dq"][t] = scale * (state @ d_out[t][:, :, None])[..., 0]
+        r["state"][i] = state
+        if d_out is None:
+            continue
+        grad = torch.zeros_like(state) if d_state is None else d_state[i].clone()
+        for t, was in zip(reversed(order), reversed(before)):
+            grad = grad + scale * Q[t][:, :, None] * d_out[t][:, None, :]
+            r["dk"][t] = (grad @ v[t][:, :, None])[..., 0]
+            r["dv"][t] = (K[t][:, None, :] @ grad)[:, 0]
+            r["dg"][t] = e[t, :, 0, 0] * (grad * was).sum((1, 2))
+            grad = e[t] * grad
+            if (t + 1 if reverse else t) in drop:
+                grad = torch.zeros_like(grad)
+        r["d_initial"][i] = grad
+    if d_out is not None:
+        r["dq"], r["dk"] = (x.view(rows, hk, group, dk).sum(2) for x in (r["dq"], r["dk"]))
+    return r
+
+
+def off(got, want):
+    """Two-norm of the difference over the two-norm of what is wanted."""
+    return ((got.double().cpu() - want).norm() / want.norm()).item()
+
+
+# What two-norms may be off.  An output's own rounding, those of the pairs' weights and of the operands are each at most half
+# a step, u = HALF[type], and evenly spread over it, so u / sqrt(3) in the two-norm: three of them u.  fp32 sums: at most some
+# 250 roundings of 2^-24 in a row (a chunk's products and rows, the steps of a chain), 2^-16 of the magnitudes, which signs at
+# random leave a small multiple of in the two-norm.
+NORM_FP32 = 2.0 ** -14
+NORM = {torch.float32: NORM_FP32, torch.bfloat16: 2.0 ** -8 + NORM_FP32, torch.float16: 2.0 ** -11 + NORM_FP32}
