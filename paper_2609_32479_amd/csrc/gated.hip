@@ -97,7 +97,7 @@ template <class T, bool GELU> __device__ __forceinline__ void act_of(float a, fl
         v = a * p;
         d = p + a * (0.3989422804014327f * e);
     } else if constexpr (GELU) {
-        const float p = 0.5f * (1.0f + erff(a * 0.70710678118654752f));
+        const float p = 0.5f * erfcf(a * -0.70710678118654752f);  // (1 + erf would lose the negative tail's digits)
         v = a * p;
         d = p + a * (0.3989422804014327f * expf(-0.5f * a * a));
     } else {
