@@ -20,7 +20,7 @@ def tf():
     return tf
 
 
-@pytest.mark.parametrize("dtype", [FP32])
+@pytest.mark.parametrize("dtype", [BF16, FP32, FP16])
 @pytest.mark.parametrize("rows", [40, 700])   # weights streamed to registers; tiles
 def test_gelu_of_far_negative_gates(tf, dtype, rows):
     # fp16's smallest normal value is 6e-5: there the other factor is large, and the gate not as far out
