@@ -462,6 +462,8 @@ typedef enum { TF_ELEM_FP32 = 0, TF_ELEM_BF16 = 1, TF_ELEM_FP16 = 2 } tf_elem;
  * the weights exp(b_t - b_s) q_t k_s of the values inside a chunk of 64 rows are
  * rounded to bf16.  fp16: as fp32, rounded once at the store.
  * A value that is infinite or NaN reaches the later rows of its own sequence only.
+ * (bf16: the row of an infinite query, for dq, dk and dv of an infinite d_out, v or k, is NaN where the formula may have
+ * infinities.)
  */
 typedef struct {
     int32_t elem;        /* tf_elem of q, k, v, out and their gradients */

@@ -84,8 +84,9 @@ struct MatBF16 {
         return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     }
     static constexpr int TILES = 2;  // state tiles of 16 rows in a fragment
-    // fp32 values as N bf16 parts, each the rest rounded: three hold all 24 bits, two 16 (and sign)
-    template <int N> static __device__ __forceinline__ void split(const float *x, F (&p)[N]) {
+    // fp32 values as N bf16 parts, each the rest rounded: three hold all 24 bits, two 16 (and sign).  WILD: values may be infinite,
+    // which have no rest
+    template <int N, bool WILD> static __device__ __forceinline__ void split(const float *x, F (&p)[N]) {
         typedef float f2 __attribute__((ext_vector_type(2)));
         typedef __bf16 b2 __attribute__((ext_vector_type(2)));
         o_u32x4 w[N];
@@ -97,6 +98,9 @@ struct MatBF16 {
                 const unsigned u = __builtin_bit_cast(unsigned, __builtin_convertvector(r, b2));
                 w[j][i] = u;
                 if (j + 1 < N) r = f2{r[0] - __uint_as_float(u << 16), r[1] - __uint_as_float(u & 0xffff0000u)};
+                if (WILD && j == 0)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) r[h] = __builtin_amdgcn_fmed3f(r[h], 0.0f, r[h]);  // NaN: the other operand
             }
         }
 #pragma unroll
@@ -125,7 +129,7 @@ struct MatF32 {
         return along(x, ld, row, k0, q);
     }
     static constexpr int TILES = 1;
-    template <int N> static __device__ __forceinline__ void split(const float *x, F (&p)[N]) {
+    template <int N, bool WILD> static __device__ __forceinline__ void split(const float *x, F (&p)[N]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[0][i] = x[i];
     }
@@ -649,7 +653,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                                                      float x[4 * M::TILES];
 #pragma unroll
                                                      for (int e = 0; e < 4 * M::TILES; ++e) x[e] = S[j][k * M::TILES + e / 4][e % 4];
-                                                     M::template split<NS>(x, sp[j]);
+                                                     M::template split<NS, true>(x, sp[j]);
                                                  }
                                              }
                                              // (a branch costs more than the bf16 products of rows that are not the sequence's)
@@ -700,7 +704,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                                 const int s = k * KM + KM / 4 * q + i;
                                 x[i] = s >= a && s < b ? (float)v[i] * w[i] : 0.0f;
                             }
-                            M::template split<NU>(x, vp[j]);
+                            M::template split<NU, false>(x, vp[j]);
                         }
                         in_turn<ST, 3>([&](int m) { return M::down(Ks, LK, k * KM, 16 * m, n, q); },
                                        [&](int m, F kf) {
