@@ -473,6 +473,8 @@ typedef struct {
     int32_t d_v;
     int32_t reverse;     /* 0 or 1 */
     float scale;
+    int32_t clear;       /* outputs whose rows outside of all sequences become zeros, a bit each: 1 out; backward 1 dq, 2 dk, 4 dv,
+                          * 8 d_log_decay (0: no such row is written) */
 } tf_decay_config;
 
 /* Bytes of workspace of tf_decay_attention and of its backward pass (0 if invalid). */
@@ -491,7 +493,7 @@ size_t tf_decay_backward_workspace_size(const tf_decay_config *cfg, int64_t n_ro
  *                every output NaN.
  * initial_state  device, float32 [n_seqs][n_heads][d_k][d_v], or NULL for zeros.
  * out            device, [n_rows][n_heads][d_v].  Rows outside of all sequences are
- *                not written.
+ *                not written, or zeros (cfg->clear).
  * final_state    device, float32, as initial_state, or NULL.  A sequence without
  *                rows passes its initial state on.
  * flags          device int32 or NULL, OR-ed.
@@ -507,7 +509,8 @@ tf_status tf_decay_attention(const tf_decay_config *cfg, const void *q, int64_t 
  * d_state as final_state (NULL: the last states are not used).  dq, dk, dv as q, k, v
  * (queries and keys that heads share get the sum); d_log_decay float32
  * [n_rows][n_heads], or [n_heads] with decay_stride 0 (the sum over all rows);
- * d_initial as initial_state, or NULL.  Other arguments are those of the forward call.
+ * d_initial as initial_state, or NULL.  Rows outside of all sequences are not written, or
+ * zeros (cfg->clear).  Other arguments are those of the forward call.
  */
 tf_status tf_decay_attention_backward(const tf_decay_config *cfg, const void *d_out, int64_t d_out_stride, const void *q,
                                       int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,

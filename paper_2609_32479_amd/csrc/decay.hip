@@ -827,6 +827,16 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
     }
 }
 
+// Outputs whose rows outside of all sequences become zeros: p null where they are left as they are.
+struct DecayClear {
+    char *p[4];
+    long long stride[4];  // bytes
+    int words[4];         // of a row, 4 bytes each
+    void add(int i, void *x, int64_t row_stride, int64_t width, size_t size) {
+        p[i] = (char *)x, stride[i] = row_stride * (int64_t)size, words[i] = (int)(width * (int64_t)size / 4);
+    }
+};
+
 // First and past-the-last row of every row's sequence; whether the offsets are in order and inside the array.  A workgroup
 // has 1024 rows: it finds the sequence of the first by 256 probes at a time, puts the starts of the sequences that follow
 // where they are, and a running maximum tells every row its sequence (a thread a row and a binary search each took 92 us
@@ -835,7 +845,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
 __global__ __launch_bounds__(256) void tf_decay_index_kernel(const int32_t *__restrict__ offsets, int n_seqs, int n_rows,
                                                              int2 *__restrict__ info, int *__restrict__ bad,
                                                              int32_t *__restrict__ flags, long long size, int per,
-                                                             const float *__restrict__ s0, float *__restrict__ sf) {
+                                                             const float *__restrict__ s0, float *__restrict__ sf, DecayClear C) {
     __shared__ int mark[kIndexRows], top[4];
     const int tid = threadIdx.x;
     if (blockIdx.x < kCheckers) {
@@ -867,6 +877,7 @@ __global__ __launch_bounds__(256) void tf_decay_index_kernel(const int32_t *__re
         return;
     }
     const int r0 = tile * kIndexRows, r1 = n_rows - r0 < kIndexRows ? n_rows : r0 + kIndexRows;
+    const int first = offsets[0], last = offsets[n_seqs];
     // how many of the n_seqs + 1 offsets are at most r0
     int lo = 0, hi = n_seqs + 1;
     while (lo < hi) {
@@ -905,6 +916,14 @@ __global__ __launch_bounds__(256) void tf_decay_index_kernel(const int32_t *__re
         const int r = r0 + 4 * tid + j, k = m[j] > before ? m[j] : before;
         if (r < n_rows) info[r] = k == 0 || k > n_seqs ? int2{-1, -1} : int2{offsets[k - 1], offsets[k]};
     }
+    // The tile's rows before the first sequence and behind the last.
+    if (first <= r0 && last >= r1) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (C.p[i])
+            for (int r = r0 + tid / 64; r < r1; r += 4)
+                if (r < first || r >= last)
+                    for (int w = tid % 64; w < C.words[i]; w += 64) *(unsigned *)(C.p[i] + r * C.stride[i] + 4 * w) = 0;
 }
 
 // The states at the spans' ends from the spans' own contributions, in order along each cut sequence.  A wave has 128
@@ -1171,7 +1190,7 @@ __global__ __launch_bounds__(256) void tf_decay_step_kernel(const void *__restri
 tf_status decay_check(const tf_decay_config *c) {
     if (!c || !elem_ok(c->elem) || c->n_heads < 1 || c->n_qk_heads < 1 || c->n_heads % c->n_qk_heads || c->d_k < 1 || c->d_v < 1)
         return TF_EINVAL;
-    if (!std::isfinite(c->scale) || (c->reverse != 0 && c->reverse != 1)) return TF_EINVAL;
+    if (!std::isfinite(c->scale) || (c->reverse != 0 && c->reverse != 1) || c->clear < 0 || c->clear > 15) return TF_EINVAL;
     auto width = [](int d) { return d == 32 || d == 64 || d == 128; };
     if (!width(c->d_k) || !width(c->d_v) || c->n_heads > 1024) return TF_EUNSUPPORTED;
     return TF_OK;
@@ -1278,10 +1297,10 @@ void chain_run(int elem, DecayRuns R, int runs, int dk, int dv, hipStream_t s) {
 }
 // (s0, sf: the states of `size` values that sequences without rows pass through; sf null: none)
 void index_run(const int32_t *offsets, int n_seqs, int64_t n_rows, const Plan &p, int32_t *flags, long long size, const float *s0,
-               float *sf, hipStream_t s) {
+               float *sf, const DecayClear &clear, hipStream_t s) {
     const int64_t per = ((int64_t)n_seqs + 1023) / 1024, states = sf && per ? (n_seqs + per - 1) / per : 0;
     hipLaunchKernelGGL(tf_decay_index_kernel, dim3((unsigned)(kCheckers + (n_rows + kIndexRows - 1) / kIndexRows + states)), dim3(256), 0, s,
-                       offsets, n_seqs, (int)n_rows, p.info, p.bad, flags, size, (int)per, s0, sf);
+                       offsets, n_seqs, (int)n_rows, p.info, p.bad, flags, size, (int)per, s0, sf, clear);
 }
 void last_run(int elem, const DecayGrad &G, const DecayShare &S, hipStream_t s) {
     const dim3 grid((unsigned)((G.spans.n * G.heads + 3) / 4 + 2 * S.blocks)), block(256);
@@ -1327,7 +1346,7 @@ extern "C" tf_status tf_decay_attention(const tf_decay_config *c, const void *q,
         !stride_ok(out_stride, vw, c->elem))
         return TF_EINVAL;
     if (!decay_sizes_ok(c, n_rows, n_seqs) || !strides_fit({q_stride, k_stride, v_stride, out_stride})) return TF_EUNSUPPORTED;
-    if (n_seqs == 0) return TF_OK;
+    if (n_seqs == 0 && !(c->clear && n_rows > 0)) return TF_OK;
     if (!offsets || !workspace) return TF_EINVAL;
     if (n_rows > 0 && (!q || !k || !v || !out || !log_decay)) return TF_EINVAL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(initial_state) || !aligned16(final_state) ||
@@ -1337,8 +1356,10 @@ extern "C" tf_status tf_decay_attention(const tf_decay_config *c, const void *q,
     if (over_inputs({out, final_state}, {initial_state})) return TF_EINVAL;
     const Plan p = decay_plan(c, n_rows, n_seqs, false, false, workspace);
     if (workspace_bytes < p.bytes) return TF_EINVAL;
-    index_run(offsets, n_seqs, n_rows, p, flags, (long long)c->n_heads * c->d_k * c->d_v, initial_state, final_state, stream);
-    if (n_rows > 0 || final_state) {
+    DecayClear clear = {};
+    if (c->clear & 1) clear.add(0, out, out_stride, vw, elem_bytes(c->elem));
+    index_run(offsets, n_seqs, n_rows, p, flags, (long long)c->n_heads * c->d_k * c->d_v, initial_state, final_state, clear, stream);
+    if (n_seqs > 0 && (n_rows > 0 || final_state)) {
         DecayRun A = {};
         const int group = c->n_heads / c->n_qk_heads;
         A.q = q, A.k = k, A.v = v, A.qs = q_stride, A.ks = k_stride, A.vs = v_stride;
@@ -1385,7 +1406,12 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
     const Plan p = decay_plan(c, n_rows, n_seqs, true, d_state != nullptr, workspace);
     if (workspace_bytes < p.bytes) return TF_EINVAL;
     const int H = c->n_heads, group = H / c->n_qk_heads, dir = c->reverse ? -1 : 1, size = c->d_k * c->d_v;
-    index_run(offsets, n_seqs, n_rows, p, flags, (long long)H * size, d_state, d_initial, stream);
+    DecayClear clear = {};
+    if (c->clear & 1) clear.add(0, dq, dq_stride, qw, elem_bytes(c->elem));
+    if (c->clear & 2) clear.add(1, dk, dk_stride, qw, elem_bytes(c->elem));
+    if (c->clear & 4) clear.add(2, dv, dv_stride, vw, elem_bytes(c->elem));
+    if ((c->clear & 8) && decay_stride) clear.add(3, d_log_decay, H, H, 4);
+    index_run(offsets, n_seqs, n_rows, p, flags, (long long)H * size, d_state, d_initial, clear, stream);
     DecayShare S = {};
     DecayRun A = {};
     A.group = group, A.g = log_decay, A.gs = decay_stride;

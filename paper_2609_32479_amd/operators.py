@@ -27,7 +27,7 @@ _vp, _i64, _i32, _sz, _f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ct
 
 class DecayConfig(ctypes.Structure):
     _fields_ = [("elem", _i32), ("n_heads", _i32), ("n_qk_heads", _i32), ("d_k", _i32), ("d_v", _i32),
-                ("reverse", _i32), ("scale", _f32)]
+                ("reverse", _i32), ("scale", _f32), ("clear", _i32)]
 
 
 class QKNormConfig(ctypes.Structure):
@@ -231,8 +231,9 @@ def _state(name: str, s, like: torch.Tensor, n: int, heads: int, dk: int, dv: in
         raise ValueError(f"{name} must be contiguous float32 of shape [{n}, {heads}, {dk}, {dv}]")
 
 
-def _decay_inputs(q, k, v, scale, reverse):
-    """Check q, k, v; returns the configuration and their row strides."""
+def _decay_inputs(q, k, v, scale, reverse, *outputs):
+    """Check q, k, v; returns the configuration and their row strides.  Of the outputs, those that the call allocates (None)
+    get zeros in the rows outside of all sequences."""
     elem = _elem(q)
     if q.dim() != 3 or not isinstance(v, torch.Tensor) or v.dim() != 3:
         raise ValueError("q, k and v must have shape [rows, heads, width]")
@@ -240,7 +241,8 @@ def _decay_inputs(q, k, v, scale, reverse):
     heads, dv = v.shape[1], v.shape[2]
     strides = (_rows3("q", q, q), _rows3("k", k, q, rows, qk_heads, dk), _rows3("v", v, q, rows))
     scale = dk ** -0.5 if scale is None else float(scale)
-    return _config(DecayConfig, elem, heads, qk_heads, dk, dv, int(bool(reverse)), scale), strides
+    clear = sum(1 << i for i, x in enumerate(outputs) if x is None)
+    return _config(DecayConfig, elem, heads, qk_heads, dk, dv, int(bool(reverse)), scale, clear), strides
 
 
 def decay_attention(q, k, v, log_decay, offsets, scale=None, reverse=False, initial_state=None, return_state=False,
@@ -253,12 +255,12 @@ def decay_attention(q, k, v, log_decay, offsets, scale=None, reverse=False, init
     [heads], offsets int32 [n + 1].  scale: d_k ** -0.5 by default.  reverse: from
     each sequence's last row to its first.  initial_state float32 [n, heads, d_k, d_v]
     or None.  Returns (out [rows, heads, d_v], the last states or None); rows outside
-    of all sequences are left as they are.  The last states are returned if
-    ``return_state`` is set or ``final_state`` is given.  ``flags`` (int32 GPU tensor)
-    is OR-ed with SEQ_BAD_OFFSETS when the offsets make no sequences (the outputs are
-    NaN then).
+    of all sequences are left as they are in a given ``out``, and zeros in a new one.
+    The last states are returned if ``return_state`` is set or ``final_state`` is given.
+    ``flags`` (int32 GPU tensor) is OR-ed with SEQ_BAD_OFFSETS when the offsets make no
+    sequences (the outputs are NaN then).
     """
-    (cfg, at), (qs, ks, vs) = _decay_inputs(q, k, v, scale, reverse)
+    (cfg, at), (qs, ks, vs) = _decay_inputs(q, k, v, scale, reverse, out)
     rows, n = q.shape[0], _offsets(offsets, q)
     gs = _decays(log_decay, q, rows, cfg.n_heads)
     _state("initial_state", initial_state, q, n, cfg.n_heads, cfg.d_k, cfg.d_v)
@@ -282,8 +284,10 @@ def decay_attention_backward(d_out, q, k, v, log_decay, offsets, scale=None, rev
 
     d_out as out, d_state as the last states (None: they are not used), the other
     arguments those of the forward call.  d_initial is None without an initial_state.
+    Rows outside of all sequences are zeros in the gradients that the call allocates, and
+    left as they are in given ones.
     """
-    (cfg, at), (qs, ks, vs) = _decay_inputs(q, k, v, scale, reverse)
+    (cfg, at), (qs, ks, vs) = _decay_inputs(q, k, v, scale, reverse, dq, dk, dv, d_log_decay)
     rows, n, h = q.shape[0], _offsets(offsets, q), cfg.n_heads
     gs = _decays(log_decay, q, rows, h)
     _state("initial_state", initial_state, q, n, h, cfg.d_k, cfg.d_v)
