@@ -552,6 +552,7 @@ typedef struct {
     int32_t interleaved; /* 0 or 1 */
     float eps;
     double base;
+    int32_t clear;       /* outputs whose rows outside of all sequences become zeros: 1 q_out, 2 k_out; backward 1 dq, 2 dk */
 } tf_qk_norm_config;
 
 /*
@@ -560,8 +561,8 @@ typedef struct {
  * positions device, int32 [n_rows], or NULL: then a row's position counts from its
  *           sequence's first row (offsets given) or from row 0.
  * offsets   device, int32 [n_seqs + 1], or NULL: with offsets, only rows offsets[0] ..
- *           offsets[n_seqs]-1 are read and written.  Offsets out of order give some
- *           positions no meaning.
+ *           offsets[n_seqs]-1 are read and written (the others: cfg->clear).  Offsets out
+ *           of order give some positions no meaning.
  * q_out, k_out  as q, k; may be q and k themselves (same stride).
  */
 tf_status tf_qk_norm_rotate(const tf_qk_norm_config *cfg, const void *q, int64_t q_stride, const void *k, int64_t k_stride,

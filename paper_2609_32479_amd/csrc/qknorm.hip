@@ -48,6 +48,8 @@ struct NormArgs {
     long long n_rows;
     const int32_t *positions, *offsets;
     int n_seqs, rot, tile;  // rotated values; rows of a tile
+    int clear;              // outputs (a bit each) whose rows outside of all sequences become zeros
+    int blocks;             // workgroups of the tiles
     unsigned per_head[2], per_pair;  // 2^32 over the heads, the pairs (rounded down)
     float eps;
     float *parts;  // backward: [workgroups][2][D]
@@ -98,14 +100,37 @@ template <int L> __device__ __forceinline__ float head_sum(float s) {
     return s;
 }
 
+// Zeros in the rows before the first sequence and behind the last, of the outputs that are to be cleared, a wave a row: the work
+// of the workgroups behind A.blocks (`wave` of `waves`).  Within the tiles' loop it cost the others' registers 9 % of their time.
+template <typename T, int D> __device__ __forceinline__ void norm_clear(const NormArgs &A, int wave, int waves, int lane) {
+    const long long first = A.offsets[0], last = A.offsets[A.n_seqs];
+    for (int w = 0; w < 2; ++w) {
+        if (!(A.clear >> w & 1)) continue;
+        for (long long r = wave; r < A.n_rows; r += waves) {
+            if (r >= first && r < last) {  // on to the first of this wave's rows that is behind the sequences
+                r += (last - r - 1) / waves * waves;
+                continue;
+            }
+            typename T::E *y = (typename T::E *)A.y[w] + r * A.ys[w];
+            for (int c = lane * 8; c < A.heads[w] * D; c += 512) store8<T>(y + c, o_f32x8{});
+        }
+    }
+}
+
+// (the registers' limits are those that no instance spills at)
 template <typename T, int D, bool PAIRED, bool BACK>
-__global__ __launch_bounds__(kNormBlock) void tf_qk_norm_kernel(NormArgs A, Turns turns) {
+__global__ __launch_bounds__(kNormBlock, BACK ? 3 : D <= 64 && !PAIRED ? 5 : 4) void tf_qk_norm_kernel(NormArgs A, Turns turns) {
     constexpr int L = D / 16;  // lanes of a head
     typedef typename T::E E;
     __shared__ __attribute__((aligned(16))) float cs[2 * kNormAngles];  // [row][cos, sin][pair]
     __shared__ double at[kNormRows];  // positions
     __shared__ int live[kNormRows];
     const int tid = threadIdx.x, l = tid % L;
+    if ((int)blockIdx.x >= A.blocks) {
+        norm_clear<T, D>(A, ((int)blockIdx.x - A.blocks) * (kNormBlock / 64) + tid / 64, ((int)gridDim.x - A.blocks) * (kNormBlock / 64),
+                         tid % 64);
+        return;
+    }
     const int pairs = A.rot / 2;
     const bool turned = 16 * l < A.rot;
 
@@ -121,7 +146,7 @@ __global__ __launch_bounds__(kNormBlock) void tf_qk_norm_kernel(NormArgs A, Turn
         last = e < last ? e : last;
     }
     const long long tiles = (A.n_rows + A.tile - 1) / A.tile;
-    for (long long t = blockIdx.x; t < tiles; t += gridDim.x) {
+    for (long long t = blockIdx.x; t < tiles; t += A.blocks) {
         const long long r0 = t * A.tile;
         const int rows = (int)(A.n_rows - r0 < A.tile ? A.n_rows - r0 : A.tile);
         if (r0 >= last || r0 + rows <= first) continue;
@@ -279,7 +304,7 @@ tf_status norm_check(const tf_qk_norm_config *c, int64_t n_rows, int32_t n_seqs)
     if (!elem_ok(c->elem) || c->n_q_heads < 1 || c->n_k_heads < 1 || c->head_dim < 1 || c->rotary_dim < 1 ||
         c->rotary_dim > c->head_dim)
         return TF_EINVAL;
-    if (!(c->eps >= 0.0f) || !(c->base > 0.0) || !std::isfinite(c->base) || !std::isfinite(c->eps)) return TF_EINVAL;
+    if (c->clear < 0 || c->clear > 3 || !(c->eps >= 0.0f) || !(c->base > 0.0) || !std::isfinite(c->base) || !std::isfinite(c->eps)) return TF_EINVAL;
     const int d = c->head_dim;
     if ((d != 32 && d != 64 && d != 128 && d != 256) || c->rotary_dim % 16) return TF_EUNSUPPORTED;
     if (c->n_q_heads > 1024 || c->n_k_heads > 1024 || n_rows > INT32_MAX) return TF_EUNSUPPORTED;
@@ -294,24 +319,27 @@ Turns norm_turns(const tf_qk_norm_config *c) {
 }
 
 template <typename T, int D, bool BACK>
-void norm_launch(const tf_qk_norm_config *c, const NormArgs &A, int blocks, hipStream_t stream) {
+void norm_launch(const tf_qk_norm_config *c, const NormArgs &A, hipStream_t stream) {
     const Turns t = norm_turns(c);
+    // (up to one workgroup a compute unit for the rows to clear)
+    const int64_t clear = A.clear ? (A.n_rows + 63) / 64 : 0;
+    const dim3 grid((unsigned)(A.blocks + (clear < 256 ? clear : 256)));
     if (c->interleaved)
-        hipLaunchKernelGGL((tf_qk_norm_kernel<T, D, true, BACK>), dim3(blocks), dim3(kNormBlock), 0, stream, A, t);
+        hipLaunchKernelGGL((tf_qk_norm_kernel<T, D, true, BACK>), grid, dim3(kNormBlock), 0, stream, A, t);
     else
-        hipLaunchKernelGGL((tf_qk_norm_kernel<T, D, false, BACK>), dim3(blocks), dim3(kNormBlock), 0, stream, A, t);
+        hipLaunchKernelGGL((tf_qk_norm_kernel<T, D, false, BACK>), grid, dim3(kNormBlock), 0, stream, A, t);
 }
-template <int D, bool BACK> void norm_elem(const tf_qk_norm_config *c, const NormArgs &A, int blocks, hipStream_t stream) {
-    if (c->elem == TF_ELEM_FP32) norm_launch<ElemF32, D, BACK>(c, A, blocks, stream);
-    else if (c->elem == TF_ELEM_BF16) norm_launch<ElemBF16, D, BACK>(c, A, blocks, stream);
-    else norm_launch<ElemF16, D, BACK>(c, A, blocks, stream);
+template <int D, bool BACK> void norm_elem(const tf_qk_norm_config *c, const NormArgs &A, hipStream_t stream) {
+    if (c->elem == TF_ELEM_FP32) norm_launch<ElemF32, D, BACK>(c, A, stream);
+    else if (c->elem == TF_ELEM_BF16) norm_launch<ElemBF16, D, BACK>(c, A, stream);
+    else norm_launch<ElemF16, D, BACK>(c, A, stream);
 }
-template <bool BACK> void norm_width(const tf_qk_norm_config *c, const NormArgs &A, int blocks, hipStream_t stream) {
+template <bool BACK> void norm_width(const tf_qk_norm_config *c, const NormArgs &A, hipStream_t stream) {
     switch (c->head_dim) {
-        case 32: norm_elem<32, BACK>(c, A, blocks, stream); break;
-        case 64: norm_elem<64, BACK>(c, A, blocks, stream); break;
-        case 128: norm_elem<128, BACK>(c, A, blocks, stream); break;
-        default: norm_elem<256, BACK>(c, A, blocks, stream); break;
+        case 32: norm_elem<32, BACK>(c, A, stream); break;
+        case 64: norm_elem<64, BACK>(c, A, stream); break;
+        case 128: norm_elem<128, BACK>(c, A, stream); break;
+        default: norm_elem<256, BACK>(c, A, stream); break;
     }
 }
 template <int D> void gain_launch(const tf_qk_norm_config *c, const float *parts, int n, float *dq, float *dk, hipStream_t s) {
@@ -323,7 +351,7 @@ template <int D> void gain_launch(const tf_qk_norm_config *c, const float *parts
 
 void norm_sizes(const tf_qk_norm_config *c, int64_t n_rows, NormArgs &A) {
     auto per = [](unsigned n) { return n == 1 ? 0xffffffffu : (unsigned)((1ull << 32) / n); };
-    A.rot = c->rotary_dim, A.tile = norm_tile(c, n_rows), A.eps = c->eps;
+    A.rot = c->rotary_dim, A.tile = norm_tile(c, n_rows), A.eps = c->eps, A.clear = A.offsets ? c->clear : 0;
     A.per_head[0] = per((unsigned)c->n_q_heads), A.per_head[1] = per((unsigned)c->n_k_heads), A.per_pair = per((unsigned)c->rotary_dim / 2);
 }
 bool strides_fit(std::initializer_list<int64_t> strides) {
@@ -375,7 +403,8 @@ extern "C" tf_status tf_qk_norm_rotate(const tf_qk_norm_config *c, const void *q
     A.heads[0] = c->n_q_heads, A.heads[1] = c->n_k_heads;
     A.n_rows = n_rows, A.positions = positions, A.offsets = offsets, A.n_seqs = n_seqs;
     norm_sizes(c, n_rows, A);
-    norm_width<false>(c, A, (int)norm_blocks(c, n_rows, 1 << 20), stream);
+    A.blocks = (int)norm_blocks(c, n_rows, 1 << 20);
+    norm_width<false>(c, A, stream);
     return hipGetLastError() == hipSuccess ? TF_OK : TF_EHIP;
 }
 
@@ -415,7 +444,8 @@ extern "C" tf_status tf_qk_norm_rotate_backward(const tf_qk_norm_config *c, cons
     A.parts = (float *)workspace;
     int blocks = (int)norm_blocks(c, n_rows, kNormParts);
     if (blocks < 1) blocks = 1;  // no rows: the gradients of the gains are zeros
-    norm_width<true>(c, A, blocks, stream);
+    A.blocks = blocks;
+    norm_width<true>(c, A, stream);
     switch (c->head_dim) {
         case 32: gain_launch<32>(c, A.parts, blocks, dq_gain, dk_gain, stream); break;
         case 64: gain_launch<64>(c, A.parts, blocks, dq_gain, dk_gain, stream); break;

@@ -32,7 +32,7 @@ class DecayConfig(ctypes.Structure):
 
 class QKNormConfig(ctypes.Structure):
     _fields_ = [("elem", _i32), ("n_q_heads", _i32), ("n_k_heads", _i32), ("head_dim", _i32), ("rotary_dim", _i32),
-                ("interleaved", _i32), ("eps", _f32), ("base", ctypes.c_double)]
+                ("interleaved", _i32), ("eps", _f32), ("base", ctypes.c_double), ("clear", _i32)]
 
 
 class GatedConfig(ctypes.Structure):
@@ -332,7 +332,7 @@ def decay_attention_step(q, k, v, log_decay, state, scale=None, state_out=None, 
     return out, state_out
 
 
-def _norm_inputs(q, k, q_gain, k_gain, offsets, positions, rotary_dim, base, interleaved, eps):
+def _norm_inputs(q, k, q_gain, k_gain, offsets, positions, rotary_dim, base, interleaved, eps, q_out, k_out):
     elem = _elem(q)
     if q.dim() != 3:
         raise ValueError("q and k must have shape [rows, heads, width]")
@@ -352,7 +352,8 @@ def _norm_inputs(q, k, q_gain, k_gain, offsets, positions, rotary_dim, base, int
     rot = d if rotary_dim is None else int(rotary_dim)
     if not math.isfinite(float(base)):
         raise ValueError("base must be finite")
-    return _config(QKNormConfig, elem, hq, k.shape[1], d, rot, int(bool(interleaved)), float(eps), float(base)), qs, ks, n
+    clear = int(q_out is None) | int(k_out is None) << 1 if offsets is not None else 0
+    return _config(QKNormConfig, elem, hq, k.shape[1], d, rot, int(bool(interleaved)), float(eps), float(base), clear), qs, ks, n
 
 
 def qk_norm_rotate(q, k, q_gain, k_gain, offsets=None, positions=None, rotary_dim=None, base=10000.0, interleaved=False,
@@ -364,10 +365,11 @@ def qk_norm_rotate(q, k, q_gain, k_gain, offsets=None, positions=None, rotary_di
     ``positions`` (int32 [rows]), else it counts from its sequence's first row
     (``offsets``), else from row 0.  The first ``rotary_dim`` values (default: all) are
     rotated, in pairs (j, j + rotary_dim / 2), or of neighbours if ``interleaved``.
-    With offsets only the sequences' rows are written.  ``q_out`` and ``k_out`` may be
-    q and k.
+    With offsets only the sequences' rows are written; the others are zeros in tensors
+    that the call allocates.  ``q_out`` and ``k_out`` may be q and k.
     """
-    (cfg, at), qs, ks, n = _norm_inputs(q, k, q_gain, k_gain, offsets, positions, rotary_dim, base, interleaved, eps)
+    (cfg, at), qs, ks, n = _norm_inputs(q, k, q_gain, k_gain, offsets, positions, rotary_dim, base, interleaved, eps, q_out,
+                                        k_out)
     with _on(q, stream) as s:
         q_out, qos = _rows_out("q_out", q_out, q, tuple(q.shape))
         k_out, kos = _rows_out("k_out", k_out, q, tuple(k.shape))
@@ -382,8 +384,9 @@ def qk_norm_rotate_backward(dq_out, dk_out, q, k, q_gain, k_gain, offsets=None, 
                             workspace=None, stream=None):
     """Gradients of qk_norm_rotate's inputs from those of its outputs: (dq, dk,
     dq_gain, dk_gain); q, k and the rest as in the forward call.  ``dq`` and ``dk``
-    may be ``dq_out`` and ``dk_out``."""
-    (cfg, at), qs, ks, n = _norm_inputs(q, k, q_gain, k_gain, offsets, positions, rotary_dim, base, interleaved, eps)
+    may be ``dq_out`` and ``dk_out``.  With offsets, rows outside of all sequences are
+    zeros in gradients that the call allocates and left as they are in given ones."""
+    (cfg, at), qs, ks, n = _norm_inputs(q, k, q_gain, k_gain, offsets, positions, rotary_dim, base, interleaved, eps, dq, dk)
     rows, d = q.shape[0], q.shape[2]
     dqos = _rows3("dq_out", dq_out, q, *q.shape)
     dkos = _rows3("dk_out", dk_out, q, *k.shape)

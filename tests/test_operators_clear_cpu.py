@@ -21,3 +21,9 @@ def test_decay_clear(tf, clear, fine):
     assert (tf.lib().tf_decay_workspace_size(c, 100) > 0) == fine
     none = tf.lib().tf_decay_attention(c, None, 128, None, 128, None, 128, None, 4, 0, None, 0, None, None, 0, None, 128, None, None, None)
     assert none == (tf.TF_OK if fine else tf.TF_EINVAL)
+
+
+@pytest.mark.parametrize("clear,fine", [(0, True), (3, True), (4, False), (-1, False)])
+def test_norm_clear(tf, clear, fine):
+    c = ctypes.byref(tf.QKNormConfig(1, 4, 2, 64, 64, 0, 1e-6, 1e4, clear))
+    assert (tf.lib().tf_qk_norm_workspace_size(c, 100) > 0) == fine

@@ -44,3 +44,29 @@ def test_decay_attention_in_padded_buffers(tf, dtype, qk, rows, off):
         assert not bool(x[:lo].any()) and not bool(x[hi:].any())
         assert bool((y[:lo] == -7).all()) and bool((y[hi:] == -7).all())
     assert torch.equal(mixed[1], given[2]) and all(torch.equal(mixed[i], new[i + 1]) for i in (0, 2, 3))
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32, FP16])
+@pytest.mark.parametrize("d,rot,inter", [(32, 32, False), (128, 48, True)])
+@pytest.mark.parametrize("rows,off", [(3000, [500, 520, 520, 1300]), (70, [0, 20, 33]), (50, [50, 50]), (40, [7])])
+def test_norm_rotate_in_padded_buffers(tf, dtype, d, rot, inter, rows, off):
+    r = lambda *s: torch.randn(*s, device="cuda").to(dtype)  # noqa: E731
+    q, k, dq, dk = r(rows, 3, d), r(rows, 2, d), r(rows, 3, d), r(rows, 2, d)
+    gain, o = torch.rand(d, device="cuda") + 0.5, torch.tensor(off, dtype=torch.int32, device="cuda")
+    lo, hi = off[0], off[-1]
+    for x in (q, k, dq, dk):
+        x[:lo], x[hi:] = float("nan"), float("nan")
+    mark = lambda x: torch.full_like(x, -7.0)  # noqa: E731
+    how = dict(offsets=o, rotary_dim=rot, interleaved=inter)
+    _used_memory()
+    back = tf.qk_norm_rotate_backward(dq, dk, q, k, gain, gain, **how)
+    new = (*tf.qk_norm_rotate(q, k, gain, gain, **how), *back[:2])
+    other = tf.qk_norm_rotate_backward(dq, dk, q, k, gain, gain, dq=mark(q), dk=mark(k), **how)
+    given = (*tf.qk_norm_rotate(q, k, gain, gain, q_out=mark(q), k_out=mark(k), **how), *other[:2])
+    for x, y in zip(new, given):
+        assert torch.equal(x[lo:hi], y[lo:hi]) and bool(torch.isfinite(x).all())
+        assert not bool(x[:lo].any()) and not bool(x[hi:].any())
+        assert bool((y[:lo] == -7).all()) and bool((y[hi:] == -7).all())
+    assert all(torch.equal(a, b) and bool(torch.isfinite(a).all()) for a, b in zip(back[2:], other[2:]))
+    mixed = tf.qk_norm_rotate(q, k, gain, gain, k_out=mark(k), **how)
+    assert torch.equal(mixed[0], new[0]) and torch.equal(mixed[1], given[1])
