@@ -6,6 +6,11 @@ tensors, allocates the outputs and the workspace that the caller did not pass, a
 enqueues the HIP kernels on ``stream`` (default: the tensors' device's current
 stream).  What it allocates belongs to that stream, so that a workspace that is
 freed when the function returns is not used by other streams' work too early.
+
+The functions record nothing for autograd.  With gradients enabled the forward calls
+refuse tensors that require one, whose gradients would silently be lost: call them under
+``torch.no_grad()`` and take the gradients from the ``_backward`` functions, whose own
+results have no graph either.
 """
 from __future__ import annotations
 
@@ -138,6 +143,16 @@ def _elem(x) -> int:
     return _ELEMS[x.dtype]
 
 
+_grad_enabled = torch.is_grad_enabled
+
+
+def _no_graph(what: str, **tensors):
+    for name, x in tensors.items():
+        if x is not None and x.requires_grad:
+            raise RuntimeError(f"{what} records no gradient, and {name} requires one: call it under torch.no_grad() and take "
+                               f"gradients from the _backward function")
+
+
 def _rows3(name: str, x: torch.Tensor, like: torch.Tensor, rows=None, heads=None, width=None) -> int:
     """Check a [rows, heads, width] tensor whose rows are contiguous; returns its row stride."""
     _same(name, x, like, like.dtype)
@@ -231,9 +246,9 @@ def _state(name: str, s, like: torch.Tensor, n: int, heads: int, dk: int, dv: in
         raise ValueError(f"{name} must be contiguous float32 of shape [{n}, {heads}, {dk}, {dv}]")
 
 
-def _decay_inputs(q, k, v, scale, reverse, *outputs):
-    """Check q, k, v; returns the configuration and their row strides.  Of the outputs, those that the call allocates (None)
-    get zeros in the rows outside of all sequences."""
+def _decay_inputs(q, k, v, scale, reverse, clear=0):
+    """Check q, k, v; returns the configuration and their row strides.  clear: the outputs, a bit each, that get zeros in
+    the rows outside of all sequences (those that the call allocates)."""
     elem = _elem(q)
     if q.dim() != 3 or not isinstance(v, torch.Tensor) or v.dim() != 3:
         raise ValueError("q, k and v must have shape [rows, heads, width]")
@@ -241,7 +256,6 @@ def _decay_inputs(q, k, v, scale, reverse, *outputs):
     heads, dv = v.shape[1], v.shape[2]
     strides = (_rows3("q", q, q), _rows3("k", k, q, rows, qk_heads, dk), _rows3("v", v, q, rows))
     scale = dk ** -0.5 if scale is None else float(scale)
-    clear = sum(1 << i for i, x in enumerate(outputs) if x is None)
     return _config(DecayConfig, elem, heads, qk_heads, dk, dv, int(bool(reverse)), scale, clear), strides
 
 
@@ -260,11 +274,14 @@ def decay_attention(q, k, v, log_decay, offsets, scale=None, reverse=False, init
     ``flags`` (int32 GPU tensor) is OR-ed with SEQ_BAD_OFFSETS when the offsets make no
     sequences (the outputs are NaN then).
     """
-    (cfg, at), (qs, ks, vs) = _decay_inputs(q, k, v, scale, reverse, out)
+    (cfg, at), (qs, ks, vs) = _decay_inputs(q, k, v, scale, reverse, int(out is None))
     rows, n = q.shape[0], _offsets(offsets, q)
     gs = _decays(log_decay, q, rows, cfg.n_heads)
     _state("initial_state", initial_state, q, n, cfg.n_heads, cfg.d_k, cfg.d_v)
     _flags(flags, q)
+    if _grad_enabled():
+        _no_graph("decay_attention", q=q, k=k, v=v, log_decay=log_decay, initial_state=initial_state, out=out,
+                  final_state=final_state)
     with _on(q, stream) as s:
         out, os = _rows_out("out", out, q, (rows, cfg.n_heads, cfg.d_v))
         if return_state or final_state is not None:
@@ -287,7 +304,8 @@ def decay_attention_backward(d_out, q, k, v, log_decay, offsets, scale=None, rev
     Rows outside of all sequences are zeros in the gradients that the call allocates, and
     left as they are in given ones.
     """
-    (cfg, at), (qs, ks, vs) = _decay_inputs(q, k, v, scale, reverse, dq, dk, dv, d_log_decay)
+    clear = (dq is None) | (dk is None) << 1 | (dv is None) << 2 | (d_log_decay is None) << 3
+    (cfg, at), (qs, ks, vs) = _decay_inputs(q, k, v, scale, reverse, clear)
     rows, n, h = q.shape[0], _offsets(offsets, q), cfg.n_heads
     gs = _decays(log_decay, q, rows, h)
     _state("initial_state", initial_state, q, n, h, cfg.d_k, cfg.d_v)
@@ -322,6 +340,9 @@ def decay_attention_step(q, k, v, log_decay, state, scale=None, state_out=None, 
     if state is None:
         raise ValueError("state must be a GPU tensor")
     _state("state", state, q, n, cfg.n_heads, cfg.d_k, cfg.d_v)
+    if _grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or log_decay.requires_grad or
+                            state.requires_grad or out is not None or state_out is not None):
+        _no_graph("decay_attention_step", q=q, k=k, v=v, log_decay=log_decay, state=state, out=out, state_out=state_out)
     with _on(q, stream) as s:
         out, os = _rows_out("out", out, q, (n, cfg.n_heads, cfg.d_v))
         if state_out is not state:  # (in place: checked above)
@@ -370,6 +391,9 @@ def qk_norm_rotate(q, k, q_gain, k_gain, offsets=None, positions=None, rotary_di
     """
     (cfg, at), qs, ks, n = _norm_inputs(q, k, q_gain, k_gain, offsets, positions, rotary_dim, base, interleaved, eps, q_out,
                                         k_out)
+    if _grad_enabled() and (q.requires_grad or k.requires_grad or q_gain.requires_grad or k_gain.requires_grad or
+                            q_out is not None or k_out is not None):
+        _no_graph("qk_norm_rotate", q=q, k=k, q_gain=q_gain, k_gain=k_gain, q_out=q_out, k_out=k_out)
     with _on(q, stream) as s:
         q_out, qos = _rows_out("q_out", q_out, q, tuple(q.shape))
         k_out, kos = _rows_out("k_out", k_out, q, tuple(k.shape))
@@ -435,6 +459,8 @@ def gated_ffn(x, w_gate, w_up, activation="silu", out=None, stream=None):
     [inner, width], of one type (fp32, bf16, fp16); activation "silu" or "gelu" (a
     Phi(a)).  Returns [rows, inner]."""
     (cfg, at), xs, ws = _gated_inputs(x, w_gate, w_up, activation)
+    if _grad_enabled() and (x.requires_grad or w_gate.requires_grad or w_up.requires_grad or out is not None):
+        _no_graph("gated_ffn", x=x, w_gate=w_gate, w_up=w_up, out=out)
     with _on(x, stream) as s:
         if out is None:
             out = x.new_empty((x.shape[0], cfg.inner))
