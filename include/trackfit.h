@@ -459,8 +459,9 @@ typedef enum { TF_ELEM_FP32 = 0, TF_ELEM_BF16 = 1, TF_ELEM_FP16 = 2 } tf_elem;
  * Supported: d_k and d_v 32, 64 or 128, up to 1024 heads, row strides up to 2^24, up
  * to 2^31 - 2^16 rows and sequences; a single step: fewer than 2^24 states.
  * fp32 tensors: products and sums in fp32.  bf16: states, decays and sums in fp32;
- * the weights exp(b_t - b_s) q_t k_s of the values inside a chunk of 64 rows are
- * rounded to bf16.  fp16: as fp32, rounded once at the store.
+ * in the outputs' products states and weights exp(b_t - b_s) q_t k_s enter with 16 bits
+ * (two bf16 parts, 2^-17), those of d_log_decay and the states with all 24.  fp16: as
+ * fp32, rounded once at the store.
  * A value that is infinite or NaN reaches the later rows of its own sequence only.
  * (bf16: the row of an infinite query, for dq, dk and dv of an infinite d_out, v or k, is NaN where the formula may have
  * infinities.)

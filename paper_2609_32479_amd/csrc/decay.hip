@@ -35,11 +35,12 @@
 // cuts a sequence and these two launches end at once.
 //
 // Numbers.  bf16 tensors: the products q k^T, and the states' products, take bf16
-// operands that are the tensors themselves, or fp32 values as three bf16 parts (two
-// where the result is only rounded to bf16), so that states, decays and everything
-// that reaches the decays' gradient are fp32; the weights exp(b_t - b_s) (q_t k_s)
-// are rounded once to bf16 to multiply v.  fp32 and fp16 tensors are multiplied by the
-// fp32 instruction.
+// operands that are the tensors themselves, or fp32 values as bf16 parts: three in
+// states and in everything that reaches the decays' gradient (all 24 bits), two
+// (2^-17 of them is lost) where the result is only rounded to bf16, the states and the
+// weights exp(b_t - b_s) (q_t k_s) of the outputs.  (Weights of one part: 65 536 tracks
+// 344 us for 358, but outputs off by a quarter to two fifths more than their rounding.)
+// fp32 and fp16 tensors are multiplied by the fp32 instruction.
 #include "ops.h"
 
 #include <cmath>
@@ -387,8 +388,9 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
     constexpr int NB = kChunk / KM;                // fragments along a chunk's rows
     constexpr int NS = parts_of<M>(DOT ? 3 : 2);   // parts of the state in its product with q
     constexpr int NU = parts_of<M>(3);             // parts of the weighted v in the state's update
+    constexpr int NP = parts_of<M>(2);             // parts of the weights
     __shared__ __attribute__((aligned(16))) ME Qs[OUT ? kChunk * LK : 8], Ks[kChunk * LK], Vs[kChunk * LV],
-        Xs[DOT ? kChunk * LV : 8], Ps[OUT ? PSIZE : 8];
+        Xs[DOT ? kChunk * LV : 8], Ps[OUT ? NP * PSIZE : 8];
     __shared__ ChunkRows rows_of[2];
     __shared__ int wild[2];
     __shared__ double rowp[DOT ? 10 : 1][16], colp[DOT ? 10 : 1][16];  // of the weights' tiles, by tile_at
@@ -543,7 +545,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         if (chunks > 1) fetch_rows(1);
     }
     if (OUT)  // the weights above the diagonal that share a fragment with some below
-        for (int i = tid; i < PSIZE * (int)sizeof(ME) / 4; i += NT) ((unsigned *)Ps)[i] = 0;
+        for (int i = tid; i < NP * PSIZE * (int)sizeof(ME) / 4; i += NT) ((unsigned *)Ps)[i] = 0;
     __syncthreads();
     put(0);
     __syncthreads();
@@ -597,7 +599,14 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                         a[i] = s + i <= t && s + i >= f ? a[i] * (e * sc) : 0.0f;
                     }
                 }
-                *(V4 *)(Ps + p_at(mt) + n * p_ld(mt) + s) = __builtin_convertvector(a, V4);
+                const V4 high = __builtin_convertvector(a, V4);
+                *(V4 *)(Ps + p_at(mt) + n * p_ld(mt) + s) = high;
+                if constexpr (NP == 2) {
+                    o_f32x4 low = a - __builtin_convertvector(high, o_f32x4);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) low[i] = __builtin_amdgcn_fmed3f(low[i], 0.0f, low[i]);
+                    *(V4 *)(Ps + PSIZE + p_at(mt) + n * p_ld(mt) + s) = __builtin_convertvector(low, V4);
+                }
                 if (pairs) {
                     // products of dq's weights with q k: their sums by t and by s are what q dq and k dk have of them.  In fp64: the
                     // decays' gradient is a sum of these over a span, in which all pairs but the few around a row cancel
@@ -760,15 +769,15 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
 #pragma unroll
                 for (int m = 0; m < TM; ++m)
                     from[m] = KM == 16 ? seg_first(__builtin_amdgcn_readfirstlane(W.seg[16 * row_tile(m)])) : 0;
-                in_turn<NB * TM, 4>(
+                in_turn<NB * TM * NP, 4>(
                     [&](int i) {
                         F f = {};
-                        const int mt = row_tile(i % TM);
-                        if (i / TM * KM <= 16 * mt) f = M::along(Ps + p_at(mt), p_ld(mt), n, i / TM * KM, q);
+                        const int mt = row_tile(i / NP % TM), k = i / NP / TM, part = NP - 1 - i % NP;
+                        if (k * KM <= 16 * mt) f = M::along(Ps + part * PSIZE + p_at(mt), p_ld(mt), n, k * KM, q);
                         return f;
                     },
                     [&](int i, F f) {
-                        const int k = i / TM, m = i % TM;
+                        const int k = i / NP / TM, m = i / NP % TM;
                         if (k * KM <= 16 * row_tile(m) && (KM == 32 || k * KM + KM > from[m])) {
 #pragma unroll
                             for (int j = 0; j < CT; ++j) o[j][m] = M::mma(vf[k][j], f, o[j][m]);
@@ -784,7 +793,12 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                         for (int j = 0; j < CT; ++j)
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
-                                o[j][m][i] += (float)Ps[p_at(row_tile(m)) + n * p_ld(row_tile(m)) + s] * (float)Vs[s * LV + c0 + 16 * j + 4 * q + i];
+                            {
+                                const ME *w = Ps + p_at(row_tile(m)) + n * p_ld(row_tile(m)) + s;
+                                float p = (float)w[0];
+                                if constexpr (NP == 2) p += (float)w[PSIZE];
+                                o[j][m][i] += p * (float)Vs[s * LV + c0 + 16 * j + 4 * q + i];
+                            }
                 }
             }
             // (the chunk's first row is a scalar; 64 rows of a stride fit in 32 bits)
