@@ -95,6 +95,9 @@ def _check(status: int, what: str):
 def _config(kind, *fields):
     """A configuration of these plain values and a pointer to it (the library only reads it)."""
     cfg = kind(*fields)
+    for (name, of), x in zip(kind._fields_, fields):  # ctypes keeps an int's low bits
+        if of is _i32 and getattr(cfg, name) != x:
+            raise ValueError(f"{name} {x} is not a 32-bit number")
     return cfg, ctypes.byref(cfg)
 
 

@@ -1,0 +1,30 @@
+"""The binding's own checks, on the CPU: tensors of the meta device stand in for the GPU's."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture
+def operators(monkeypatch):
+    from paper_2609_32479_amd import operators
+    monkeypatch.setattr(operators, "_same", lambda *a, **k: None)
+    monkeypatch.setattr(operators, "_elem", lambda x: 1)
+    return operators
+
+
+def _meta(*shape):
+    return torch.empty(*shape, device="meta")
+
+
+def test_sizes_past_32_bits_are_refused(operators):
+    w = _meta(2 ** 32 + 5, 8)   # would count as 5 inner values
+    with pytest.raises(ValueError, match="inner 4294967301"):
+        operators._gated_inputs(_meta(3, 8), w, w, "silu")
+    x = _meta(4, 2, 64)
+    with pytest.raises(ValueError, match="rotary_dim"):
+        operators._norm_inputs(x, x, _meta(64), _meta(64), None, None, 2 ** 32 + 64, 1e4, False, 1e-6, None, None)
+    with pytest.raises(ValueError, match="n_q_heads"):
+        operators._norm_inputs(_meta(1, 2 ** 32 + 2, 64), x[:1], _meta(64), _meta(64), None, None, 64, 1e4, False, 1e-6, None, None)
+    with pytest.raises(ValueError, match="n_heads"):
+        operators._decay_inputs(x[:1], x[:1], _meta(1, 2 ** 32 + 2, 32), None, False)
+    assert operators._gated_inputs(_meta(3, 8), _meta(5, 8), _meta(5, 8), "silu")[0][0].inner == 5
