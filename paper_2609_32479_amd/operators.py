@@ -112,14 +112,19 @@ class _On:
         index, stream = self.tensor.get_device(), self.stream
         if stream is None and index == torch._C._cuda_getDevice():  # nothing to switch
             return torch._C._cuda_getCurrentRawStream(index)
-        self.stack = contextlib.ExitStack()
-        self.stack.enter_context(torch.cuda.device(index))
-        if stream is None:
-            return int(torch.cuda.current_stream().cuda_stream)
-        if not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(int(stream))
-        self.stack.enter_context(torch.cuda.stream(stream))
-        return int(stream.cuda_stream)
+        with contextlib.ExitStack() as stack:  # (left again if something below fails)
+            stack.enter_context(torch.cuda.device(index))
+            if stream is None:
+                handle = torch.cuda.current_stream().cuda_stream
+            else:
+                if not hasattr(stream, "cuda_stream"):
+                    stream = torch.cuda.ExternalStream(int(stream))
+                if stream.device.index != index:  # (its memory and its kernels would be another device's)
+                    raise ValueError(f"the stream is on {stream.device}, the tensors on {self.tensor.device}")
+                stack.enter_context(torch.cuda.stream(stream))
+                handle = stream.cuda_stream
+            self.stack = stack.pop_all()
+        return int(handle)
 
     def __exit__(self, *exc):
         if self.stack is not None:

@@ -28,3 +28,44 @@ def test_sizes_past_32_bits_are_refused(operators):
     with pytest.raises(ValueError, match="n_heads"):
         operators._decay_inputs(x[:1], x[:1], _meta(1, 2 ** 32 + 2, 32), None, False)
     assert operators._gated_inputs(_meta(3, 8), _meta(5, 8), _meta(5, 8), "silu")[0][0].inner == 5
+
+
+class _Device:
+    """Stands in for torch.cuda.device: counts what is entered and not left."""
+    inside = 0
+
+    def __init__(self, index):
+        pass
+
+    def __enter__(self):
+        _Device.inside += 1
+
+    def __exit__(self, *exc):
+        _Device.inside -= 1
+
+
+class _Tensor:
+    device = "cuda:1"
+
+    def get_device(self):
+        return 1
+
+
+class _Stream:
+    def __init__(self, index):
+        self.device, self.cuda_stream = torch.device("cuda", index), 4096
+
+
+def test_streams_that_do_not_fit_leave_the_device_as_it_was(monkeypatch):
+    from paper_2609_32479_amd import operators
+    monkeypatch.setattr(torch.cuda, "device", _Device)
+    monkeypatch.setattr(torch.cuda, "stream", _Device)
+    monkeypatch.setattr(operators.torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    with operators._On(_Tensor(), _Stream(1)) as handle:
+        assert handle == 4096 and _Device.inside == 2
+    assert _Device.inside == 0
+    for stream, error in ((object(), TypeError), (_Stream(0), ValueError)):
+        with pytest.raises(error):
+            with operators._On(_Tensor(), stream):
+                pass
+        assert _Device.inside == 0
