@@ -263,7 +263,7 @@ def _decay_inputs(q, k, v, scale, reverse, clear=0):
     rows, qk_heads, dk = q.shape
     heads, dv = v.shape[1], v.shape[2]
     strides = (_rows3("q", q, q), _rows3("k", k, q, rows, qk_heads, dk), _rows3("v", v, q, rows))
-    scale = dk ** -0.5 if scale is None else float(scale)
+    scale = float(scale) if scale is not None else dk ** -0.5 if dk else 1.0  # (heads without a width: refused by the library)
     return _config(DecayConfig, elem, heads, qk_heads, dk, dv, int(bool(reverse)), scale, clear), strides
 
 

@@ -69,3 +69,16 @@ def test_streams_that_do_not_fit_leave_the_device_as_it_was(monkeypatch):
             with operators._On(_Tensor(), stream):
                 pass
         assert _Device.inside == 0
+
+
+def test_heads_without_a_width_reach_the_library(operators):
+    """... which refuses them with its own error."""
+    import ctypes
+    import os
+
+    import paper_2609_32479_amd as tf
+    x = _meta(4, 2, 0)
+    (cfg, _), strides = operators._decay_inputs(x, x, _meta(4, 2, 32), None, False)
+    assert (cfg.d_k, strides) == (0, (0, 0, 64))
+    if os.path.exists(tf.LIB_PATH):
+        assert tf.lib().tf_decay_workspace_size(ctypes.byref(cfg), 4) == 0
