@@ -437,8 +437,8 @@ tf_status tf_mingru_device_error(const tf_mingru *h, hipStream_t stream, int32_t
  * Tensors are row-major with unit stride inside a row ([heads][width] of a row are
  * contiguous); row strides are in elements.  Pointers of tensors and workspaces and
  * the rows' strides in bytes are multiples of 16 (workspaces of tf_decay_*: 256);
- * anything else is TF_EINVAL.  Outputs must not overlap inputs or each other unless
- * said so; one that starts where an input does is TF_EINVAL.
+ * anything else is TF_EINVAL.  Outputs and the workspace must not overlap inputs or each
+ * other unless said so; one that starts where an input or another does is TF_EINVAL.
  * All calls: TF_EINVAL (null pointers that are needed, negative sizes, strides
  * below a row's width, alignment, unknown element type, a workspace that is too
  * small), TF_EUNSUPPORTED (sizes outside the supported set), TF_EHIP.

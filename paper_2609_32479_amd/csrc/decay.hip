@@ -1367,7 +1367,8 @@ extern "C" tf_status tf_decay_attention(const tf_decay_config *c, const void *q,
         ((uintptr_t)workspace & 255))
         return TF_EINVAL;
     if (n_rows > 0 && over_inputs({out}, {q, k, v, log_decay})) return TF_EINVAL;
-    if (over_inputs({out, final_state}, {initial_state})) return TF_EINVAL;
+    if (over_inputs({out, final_state, workspace}, {initial_state}) || twice({out, final_state, workspace})) return TF_EINVAL;
+    if (over_inputs({workspace, final_state}, {q, k, v, log_decay, offsets})) return TF_EINVAL;
     const Plan p = decay_plan(c, n_rows, n_seqs, false, false, workspace);
     if (workspace_bytes < p.bytes) return TF_EINVAL;
     DecayClear clear = {};
@@ -1417,6 +1418,9 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
         return TF_EINVAL;
     if (n_rows > 0 && over_inputs({dq, dk, dv, d_log_decay}, {d_out, q, k, v, log_decay})) return TF_EINVAL;
     if (n_seqs > 0 && over_inputs({d_initial}, {initial_state, d_state})) return TF_EINVAL;
+    if (over_inputs({workspace}, {d_out, q, k, v, log_decay, offsets, initial_state, d_state}) ||
+        twice({dq, dk, dv, d_log_decay, d_initial, workspace}))
+        return TF_EINVAL;
     const Plan p = decay_plan(c, n_rows, n_seqs, true, d_state != nullptr, workspace);
     if (workspace_bytes < p.bytes) return TF_EINVAL;
     const int H = c->n_heads, group = H / c->n_qk_heads, dir = c->reverse ? -1 : 1, size = c->d_k * c->d_v;
@@ -1509,7 +1513,8 @@ extern "C" tf_status tf_decay_attention_step(const tf_decay_config *c, const voi
     if (!q || !k || !v || !log_decay || !state || !state_out || !out) return TF_EINVAL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(state) || !aligned16(state_out))
         return TF_EINVAL;
-    if (over_inputs({out}, {q, k, v, log_decay, state}) || over_inputs({state_out}, {q, k, v, log_decay})) return TF_EINVAL;
+    if (over_inputs({out}, {q, k, v, log_decay, state}) || over_inputs({state_out}, {q, k, v, log_decay}) || out == state_out)
+        return TF_EINVAL;
     const dim3 grid((unsigned)((int64_t)n_seqs * c->n_heads));
     const int group = c->n_heads / c->n_qk_heads;
 #define TF_STEP(T)                                                                                                               \

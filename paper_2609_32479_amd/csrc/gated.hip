@@ -621,7 +621,8 @@ extern "C" tf_status tf_gated_ffn_backward(const tf_gated_config *c, const void 
     if (!aligned16(x) || !aligned16(w_gate) || !aligned16(w_up) || !aligned16(dx) || !aligned16(dw_gate) || !aligned16(dw_up) ||
         !aligned16(workspace) || ((uintptr_t)d_out & (elem_bytes(c->elem) - 1)))
         return TF_EINVAL;
-    if ((n_rows > 0 && over_inputs({dx, dw_gate, dw_up}, {d_out, x})) || over_inputs({dx, dw_gate, dw_up}, {w_gate, w_up}) || dw_gate == dw_up)
+    if ((n_rows > 0 && over_inputs({dx, dw_gate, dw_up, workspace}, {d_out, x})) ||
+        over_inputs({dx, dw_gate, dw_up, workspace}, {w_gate, w_up}) || twice({dx, dw_gate, dw_up, workspace}))
         return TF_EINVAL;
     const GatedPlan p = gated_plan(c, n_rows);
     if (workspace_bytes < p.bytes) return TF_EINVAL;

@@ -87,4 +87,12 @@ inline bool over_inputs(std::initializer_list<const void *> outputs, std::initia
     return false;
 }
 
+// Whether two outputs (the workspace is one) are the same.
+inline bool twice(std::initializer_list<const void *> outputs) {
+    for (auto o = outputs.begin(); o != outputs.end(); ++o)
+        for (auto p = outputs.begin(); p != o; ++p)
+            if (*o && *o == *p) return true;
+    return false;
+}
+
 }  // namespace

@@ -424,13 +424,14 @@ extern "C" tf_status tf_qk_norm_rotate_backward(const tf_qk_norm_config *c, cons
     if (!strides_fit({q_stride, k_stride, dq_stride, dk_stride, dq_out_stride, dk_out_stride})) return TF_EUNSUPPORTED;
     if (!q_gain || !k_gain || !dq_gain || !dk_gain || !workspace || !aligned16(q_gain) || !aligned16(k_gain)) return TF_EINVAL;
     if (workspace_bytes < tf_qk_norm_workspace_size(c, n_rows) || ((uintptr_t)workspace & 3)) return TF_EINVAL;
+    if (twice({dq, dk, dq_gain, dk_gain, workspace}) || over_inputs({workspace, dq_gain, dk_gain}, {q_gain, k_gain})) return TF_EINVAL;
     if (n_rows > 0) {
         if (!q || !k || !dq_out || !dk_out || !dq || !dk) return TF_EINVAL;
         if (!aligned16(q) || !aligned16(k) || !aligned16(dq_out) || !aligned16(dk_out) || !aligned16(dq) || !aligned16(dk))
             return TF_EINVAL;
         if (in_place_elsewhere(dq_out, dq_out_stride, dq, dq_stride, n_rows) ||
             in_place_elsewhere(dk_out, dk_out_stride, dk, dk_stride, n_rows) || over_inputs({dq}, {dk_out, q, k, q_gain, k_gain}) ||
-            over_inputs({dk}, {dq_out, q, k, q_gain, k_gain}) || dq == dk)
+            over_inputs({dk}, {dq_out, q, k, q_gain, k_gain}) || over_inputs({workspace, dq_gain, dk_gain}, {dq_out, dk_out, q, k}))
             return TF_EINVAL;
     }
     NormArgs A = {};
