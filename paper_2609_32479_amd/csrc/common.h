@@ -9,6 +9,8 @@
 #include <cstddef>
 #include <cstdint>
 
+#include "dma.h"
+
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
@@ -353,24 +355,11 @@ __device__ __forceinline__ unsigned stream1_bits(unsigned long long rows) {
     return __builtin_bitreverse32(hi) >> (32 - SP);
 }
 
-// Copy of one weight stage from global memory straight into an LDS slot:
-// global_load_lds_dwordx4 moves 16 bytes per lane, 1 KiB per wave
-// instruction, into LDS at M0 + 16 * lane.  Each wave copies the pieces
-// w, w + WAVES, ...; waves with fewer pieces repeat the last one (same bytes to
-// the same place), so every wave issues exactly LPW loads per stage and can
-// wait for an older stage with a constant vmcnt.  The instruction is written
-// out because the compiler, which cannot tell the ring slots apart, would
-// otherwise wait for every such load before each LDS access; the kernel keeps
-// the count itself (wait_vmcnt).  The LDS address is an operand bound to M0,
-// so the compiler writes M0 itself and knows it is read here; the s_nop is
-// the one wait state the hardware needs between that write and the load.
-__device__ __forceinline__ void lds_dma16(const void *gsrc, unsigned lds_addr) {
-    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
-                 :
-                 : "v"(gsrc), "{m0}"(__builtin_amdgcn_readfirstlane(lds_addr))
-                 : "memory");
-}
-
+// Copy of one weight stage from global memory straight into an LDS slot (lds_dma16).
+// Each wave copies the pieces w, w + WAVES, ...; waves with fewer pieces repeat the last
+// one (same bytes to the same place), so every wave issues exactly LPW loads per stage
+// and can wait for an older stage with a constant vmcnt, which the kernel counts itself
+// (wait_vmcnt).
 // slot_lds: LDS byte address of the slot.
 template <class C>
 __device__ __forceinline__ void copy_stage(const unsigned char *stages, int s, unsigned slot_lds, int wid, int lane) {

@@ -383,7 +383,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
     auto p_ld = [](int mt) { return (16 * mt + 16 + KM - 1) / KM * KM + M::PAD; };
     auto p_at = [&](int mt) { return 16 * ((mt > 0 ? p_ld(0) : 0) + (mt > 1 ? p_ld(1) : 0) + (mt > 2 ? p_ld(2) : 0)); };
     constexpr int PSIZE = 16 * (4 * M::PAD + (KM == 32 ? 192 : 160));
-    constexpr int CT = 1, RG = DV == 32 ? 2 : 1, TM = 4 / RG;  // column tiles of a wave; waves that share them, and their row tiles
+    constexpr int RG = DV == 32 ? 2 : 1, TM = 4 / RG;  // waves that share a column tile, and their row tiles
     constexpr int ST = DK / 16;                    // state tiles of a wave's column tile
     constexpr int NB = kChunk / KM;                // fragments along a chunk's rows
     constexpr int NS = parts_of<M>(DOT ? 3 : 2);   // parts of the state in its product with q
@@ -399,7 +399,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
     const DecayRun &A = R.run[blockIdx.y];
     const bool dot = DOT && A.x, pairs = DOT && A.pairs;
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-    const int n = lane % 16, q = lane / 16, group = wave / RG, rg = wave % RG, c0 = 16 * CT * group;
+    const int n = lane % 16, q = lane / 16, group = wave / RG, rg = wave % RG, c0 = 16 * group;
     auto row_tile = [&](int m) { return RG == 1 ? m : rg ? 1 + m : 3 * m; };  // (pairs of tiles with equally long sums)
     const int p = blockIdx.x / A.heads, h = blockIdx.x % A.heads, dir = A.dir;
     const int bad = any_bad(A.bad), olo = A.offsets[0], ohi = A.offsets[A.n_seqs];
@@ -445,35 +445,29 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
     // both directions have the same ones (db's two halves are split by chunks).
     const int chunks = (hi - lo + kChunk - 1) / kChunk;
 
-    o_f32x4 S[CT][ST];
+    o_f32x4 S[ST];
     auto clear_state = [&] {
 #pragma unroll
-        for (int j = 0; j < CT; ++j)
-#pragma unroll
-            for (int m = 0; m < ST; ++m) S[j][m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int m = 0; m < ST; ++m) S[m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
     };
     clear_state();
     bool have = false;  // the state is that of the sequence that goes on
     auto load_state = [&](const float *s) {
-        const int step = A.turned ? 1 : DV, next = A.turned ? 16 * DK : 16;
+        const int step = A.turned ? 1 : DV;
         const float *e = s + (A.turned ? (c0 + n) * DK + 4 * q : 4 * q * DV + c0 + n);
 #pragma unroll
-        for (int j = 0; j < CT; ++j)
+        for (int m = 0; m < ST; ++m)
 #pragma unroll
-            for (int m = 0; m < ST; ++m)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) S[j][m][i] = e[(16 * m + i) * step + j * next];
+            for (int i = 0; i < 4; ++i) S[m][i] = e[(16 * m + i) * step];
     };
     auto save_state = [&](float *s, bool turned, float d) {
-        const int step = turned ? 1 : DV, next = turned ? 16 * DK : 16;
+        const int step = turned ? 1 : DV;
         float *e = s + (turned ? (c0 + n) * DK + 4 * q : 4 * q * DV + c0 + n);
         if (rg == 0) {
 #pragma unroll
-            for (int j = 0; j < CT; ++j)
+            for (int m = 0; m < ST; ++m)
 #pragma unroll
-                for (int m = 0; m < ST; ++m)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) e[(16 * m + i) * step + j * next] = S[j][m][i] * d;
+                for (int i = 0; i < 4; ++i) e[(16 * m + i) * step] = S[m][i] * d;
         }
     };
     if (OUT && cut_in) {
@@ -557,11 +551,8 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
         // (Behind the last chunk that chunk again: under a branch the loads are waited for where it ends.  One sequence of 32 768
         // rows, 8 heads of 128 x 128: 171 us with a branch, 157 without; 65 536 tracks 360 and 342.)
         fetch(c + 1 < chunks ? c + 1 : c);
-        F vf[NB][CT];  // the wave's columns of v, for the state and for the output
-        auto read_v = [&](int k) {
-#pragma unroll
-            for (int j = 0; j < CT; ++j) vf[k][j] = M::down(Vs, LV, k * KM, c0 + 16 * j, n, q);
-        };
+        F vf[NB];  // the wave's columns of v, for the state and for the output
+        auto read_v = [&](int k) { vf[k] = M::down(Vs, LV, k * KM, c0, n, q); };
         if (OUT) {
 #pragma unroll
             for (int k = 0; k < NB; ++k) read_v(k);
@@ -628,11 +619,9 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
             __syncthreads();
         }
 
-        o_f32x4 o[CT][TM];
+        o_f32x4 o[TM];
 #pragma unroll
-        for (int j = 0; j < CT; ++j)
-#pragma unroll
-            for (int m = 0; m < TM; ++m) o[j][m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int m = 0; m < TM; ++m) o[m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
         // The chunk's sequences, one after the other: what their state adds to their rows, and the state after them.  Those
         // that are whole in the chunk have none, unless states come in or go out.
 #pragma unroll 1
@@ -647,31 +636,24 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                 if (have) load_state(A.s0 + ((long long)seq * A.heads + h) * (DK * DV));
             }
             if (OUT && have) {
-                o_f32x4 z[CT][TM];
+                o_f32x4 z[TM];
 #pragma unroll
-                for (int j = 0; j < CT; ++j)
-#pragma unroll
-                    for (int m = 0; m < TM; ++m) z[j][m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
-                F sp[CT][NS];
+                for (int m = 0; m < TM; ++m) z[m] = o_f32x4{0.f, 0.f, 0.f, 0.f};
+                F sp[NS];
                 in_turn<DK / KM * TM, 4>([&](int i) { return M::along_state(Qs, LK, 16 * row_tile(i % TM) + n, i / TM * KM, q); },
                                          [&](int i, F f) {
                                              const int k = i / TM, m = i % TM;
                                              if (m == 0) {
+                                                 float x[4 * M::TILES];
 #pragma unroll
-                                                 for (int j = 0; j < CT; ++j) {
-                                                     float x[4 * M::TILES];
-#pragma unroll
-                                                     for (int e = 0; e < 4 * M::TILES; ++e) x[e] = S[j][k * M::TILES + e / 4][e % 4];
-                                                     M::template split<NS, true>(x, sp[j]);
-                                                 }
+                                                 for (int e = 0; e < 4 * M::TILES; ++e) x[e] = S[k * M::TILES + e / 4][e % 4];
+                                                 M::template split<NS, true>(x, sp);
                                              }
                                              // (a branch costs more than the bf16 products of rows that are not the sequence's)
                                              const int t = 16 * row_tile(m);
                                              if (KM == 16 && (t + 16 <= a || t >= b)) return;
 #pragma unroll
-                                             for (int e = NS - 1; e >= 0; --e)
-#pragma unroll
-                                                 for (int j = 0; j < CT; ++j) z[j][m] = M::mma(sp[j][e], f, z[j][m]);
+                                             for (int e = NS - 1; e >= 0; --e) z[m] = M::mma(sp[e], f, z[m]);
                                          });
 #pragma unroll
                 for (int m = 0; m < TM; ++m) {
@@ -679,18 +661,14 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                     const float f = A.out_scale * W.decay[t];
                     const bool on = t >= a && t < b;
 #pragma unroll
-                    for (int j = 0; j < CT; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[j][m][i] = on ? z[j][m][i] * f : o[j][m][i];
+                    for (int i = 0; i < 4; ++i) o[m][i] = on ? z[m][i] * f : o[m][i];
                 }
             }
             if (!ends || A.sf) {
                 if (have) {
                     const float d = W.decay[b - 1];
 #pragma unroll
-                    for (int j = 0; j < CT; ++j)
-#pragma unroll
-                        for (int m = 0; m < ST; ++m) S[j][m] *= d;
+                    for (int m = 0; m < ST; ++m) S[m] *= d;
                 } else {
                     clear_state();
                 }
@@ -700,40 +678,32 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                     for (int k = 0; k < NB; ++k) {
                         if (k * KM + KM <= a || k * KM >= b) continue;
                         if (!OUT) read_v(k);
-                        F vp[CT][NU];
+                        F vp[NU];
                         float w[KM / 4];
 #pragma unroll
                         for (int i = 0; i < KM / 4; i += 4) *(o_f32x4 *)&w[i] = *(const o_f32x4 *)&W.to[k * KM + KM / 4 * q + i];
+                        float x[KM / 4];
 #pragma unroll
-                        for (int j = 0; j < CT; ++j) {
-                            const F v = vf[k][j];
-                            float x[KM / 4];
-#pragma unroll
-                            for (int i = 0; i < KM / 4; ++i) {
-                                const int s = k * KM + KM / 4 * q + i;
-                                x[i] = s >= a && s < b ? (float)v[i] * w[i] : 0.0f;
-                            }
-                            M::template split<NU, false>(x, vp[j]);
+                        for (int i = 0; i < KM / 4; ++i) {
+                            const int s = k * KM + KM / 4 * q + i;
+                            x[i] = s >= a && s < b ? (float)vf[k][i] * w[i] : 0.0f;
                         }
+                        M::template split<NU, false>(x, vp);
                         in_turn<ST, 3>([&](int m) { return M::down(Ks, LK, k * KM, 16 * m, n, q); },
                                        [&](int m, F kf) {
 #pragma unroll
-                                           for (int i = NU - 1; i >= 0; --i)
-#pragma unroll
-                                               for (int j = 0; j < CT; ++j) S[j][m] = M::mma(kf, vp[j][i], S[j][m]);
+                                           for (int i = NU - 1; i >= 0; --i) S[m] = M::mma(kf, vp[i], S[m]);
                                        });
                     }
                 } else {
 #pragma unroll 1
-                    for (int s = a; s < b; ++s)
+                    for (int s = a; s < b; ++s) {
+                        const float v = (float)Vs[s * LV + c0 + n] * W.to[s];
 #pragma unroll
-                        for (int j = 0; j < CT; ++j) {
-                            const float v = (float)Vs[s * LV + c0 + 16 * j + n] * W.to[s];
+                        for (int m = 0; m < ST; ++m)
 #pragma unroll
-                            for (int m = 0; m < ST; ++m)
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) S[j][m][i] += (float)Ks[s * LK + 16 * m + 4 * q + i] * v;
-                        }
+                            for (int i = 0; i < 4; ++i) S[m][i] += (float)Ks[s * LK + 16 * m + 4 * q + i] * v;
+                    }
                 }
                 have = true;
                 if (ends && A.sf) {
@@ -754,12 +724,9 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                 for (int m = 0; m < TM; ++m) {
                     float z = 0.0f;
                     typedef __attribute__((ext_vector_type(4))) ME V4;
+                    const o_f32x4 x = __builtin_convertvector(*(const V4 *)(Xs + (16 * row_tile(m) + n) * LV + c0 + 4 * q), o_f32x4);
 #pragma unroll
-                    for (int j = 0; j < CT; ++j) {
-                        const o_f32x4 x = __builtin_convertvector(*(const V4 *)(Xs + (16 * row_tile(m) + n) * LV + c0 + 16 * j + 4 * q), o_f32x4);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) z += o[j][m][i] * x[i];
-                    }
+                    for (int i = 0; i < 4; ++i) z += o[m][i] * x[i];
                     z = sum_rows(z);
                     if (q == 0) dots[group][16 * row_tile(m) + n] = z;
                 }
@@ -778,27 +745,20 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                     },
                     [&](int i, F f) {
                         const int k = i / NP / TM, m = i / NP % TM;
-                        if (k * KM <= 16 * row_tile(m) && (KM == 32 || k * KM + KM > from[m])) {
-#pragma unroll
-                            for (int j = 0; j < CT; ++j) o[j][m] = M::mma(vf[k][j], f, o[j][m]);
-                        }
+                        if (k * KM <= 16 * row_tile(m) && (KM == 32 || k * KM + KM > from[m])) o[m] = M::mma(vf[k], f, o[m]);
                     });
             } else {
                 // an infinite or NaN k or v: only the products that the definition has
 #pragma unroll
                 for (int m = 0; m < TM; ++m) {
                     const int t = 16 * row_tile(m) + n, f = seg_first(W.seg[t]);
-                    for (int s = f > 0 ? f : 0; s <= t; ++s)
+                    for (int s = f > 0 ? f : 0; s <= t; ++s) {
+                        const ME *w = Ps + p_at(row_tile(m)) + n * p_ld(row_tile(m)) + s;
+                        float p = (float)w[0];
+                        if constexpr (NP == 2) p += (float)w[PSIZE];
 #pragma unroll
-                        for (int j = 0; j < CT; ++j)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                            {
-                                const ME *w = Ps + p_at(row_tile(m)) + n * p_ld(row_tile(m)) + s;
-                                float p = (float)w[0];
-                                if constexpr (NP == 2) p += (float)w[PSIZE];
-                                o[j][m][i] += p * (float)Vs[s * LV + c0 + 16 * j + 4 * q + i];
-                            }
+                        for (int i = 0; i < 4; ++i) o[m][i] += p * (float)Vs[s * LV + c0 + 4 * q + i];
+                    }
                 }
             }
             // (the chunk's first row is a scalar; 64 rows of a stride fit in 32 bits)
@@ -809,11 +769,8 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
                 const int t = 16 * row_tile(m) + n;
                 if (t < rows) {
                     char *to = ob + (unsigned)((dir > 0 ? t : rows - 1 - t) * (int)A.os + 4 * q) * (unsigned)es;
-#pragma unroll
-                    for (int j = 0; j < CT; ++j) {
-                        if (A.out_f32) *(o_f32x4 *)(to + 64 * j) = o[j][m];
-                        else store4<T>((typename T::E *)(to + 16 * j * ES), o[j][m]);
-                    }
+                    if (A.out_f32) *(o_f32x4 *)to = o[m];
+                    else store4<T>((typename T::E *)to, o[m]);
                 }
             }
         }
@@ -1329,11 +1286,7 @@ bool decay_sizes_ok(const tf_decay_config *c, int64_t n_rows, int32_t n_seqs) {
 }
 
 // A chunk's rows are addressed by 32-bit offsets.
-bool strides_fit(std::initializer_list<int64_t> strides) {
-    for (int64_t s : strides)
-        if (s > (1 << 24)) return false;
-    return true;
-}
+constexpr int64_t kFarthest = 1 << 24;
 
 }  // namespace
 
@@ -1359,7 +1312,7 @@ extern "C" tf_status tf_decay_attention(const tf_decay_config *c, const void *q,
     if (!stride_ok(q_stride, qw, c->elem) || !stride_ok(k_stride, qw, c->elem) || !stride_ok(v_stride, vw, c->elem) ||
         !stride_ok(out_stride, vw, c->elem))
         return TF_EINVAL;
-    if (!decay_sizes_ok(c, n_rows, n_seqs) || !strides_fit({q_stride, k_stride, v_stride, out_stride})) return TF_EUNSUPPORTED;
+    if (!decay_sizes_ok(c, n_rows, n_seqs) || !strides_fit({q_stride, k_stride, v_stride, out_stride}, kFarthest)) return TF_EUNSUPPORTED;
     if (n_seqs == 0 && !(c->clear && n_rows > 0)) return TF_OK;
     if (!offsets || !workspace) return TF_EINVAL;
     if (n_rows > 0 && (!q || !k || !v || !out || !log_decay)) return TF_EINVAL;
@@ -1409,7 +1362,7 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
         !stride_ok(dv_stride, vw, c->elem))
         return TF_EINVAL;
     if (!decay_sizes_ok(c, n_rows, n_seqs) ||
-        !strides_fit({q_stride, k_stride, v_stride, d_out_stride, dq_stride, dk_stride, dv_stride}))
+        !strides_fit({q_stride, k_stride, v_stride, d_out_stride, dq_stride, dk_stride, dv_stride}, kFarthest))
         return TF_EUNSUPPORTED;
     if (!offsets || !workspace || (!decay_stride && !d_log_decay)) return TF_EINVAL;
     if (n_rows > 0 && (!q || !k || !v || !d_out || !dq || !dk || !dv || !log_decay || !d_log_decay)) return TF_EINVAL;

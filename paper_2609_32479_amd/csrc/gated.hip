@@ -29,6 +29,7 @@
 // Few tokens (up to 64): reading the weights bounds it.  tf_gated_rows_kernel
 // streams them once, straight to registers, the sum dealt out to a workgroup's
 // waves (13 tokens, 1024 -> 2 x 4096: 17 MB in 5.7 us, 3 TB/s).
+#include "dma.h"
 #include "ops.h"
 
 #include <cmath>
@@ -68,19 +69,6 @@ template <> struct Mma<ElemF32> {
     }
 };
 
-__device__ __forceinline__ void dma16(const void *src, unsigned lds) {
-    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
-                 :
-                 : "v"(src), "{m0}"(__builtin_amdgcn_readfirstlane(lds))
-                 : "memory");
-}
-// The same from a scalar base and an offset for each lane.
-__device__ __forceinline__ void dma16(const char *base, unsigned off, unsigned lds) {
-    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-                 :
-                 : "v"(off), "s"(base), "{m0}"(__builtin_amdgcn_readfirstlane(lds))
-                 : "memory");
-}
 // The wave's loads into LDS have arrived and its reads are done; then the workgroup's.
 __device__ __forceinline__ void stage_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
@@ -236,26 +224,26 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tf_gated_kernel(GatedArgs A) 
         const bool whole = k0 + KS <= k_end && (ROLE != GATED_DX || f + KS <= A.F);
         if (whole) {
 #pragma unroll
-            for (int i = 0; i < LM; ++i) dma16(m, mo[i], to + i * NT * 16);
+            for (int i = 0; i < LM; ++i) lds_dma16(m, mo[i], to + i * NT * 16);
 #pragma unroll
             for (int i = 0; i < LN; ++i) {
                 // (which weight a piece is of is the same for the whole wave: 8 rows of 16, 32 or 64)
                 const bool up = NA && __builtin_amdgcn_readfirstlane((i * NT + tid) / 8 % (BN / WN)) >= BN / WN / 2;
-                dma16(up ? n2 : n, no[i], to + BM * 128 + i * NT * 16);
+                lds_dma16(up ? n2 : n, no[i], to + BM * 128 + i * NT * 16);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < LM; ++i) {
                 const void *src = m + mo[i];
                 if (k0 + mk[i] >= k_end) src = g_zeros;
-                dma16(src, to + i * NT * 16);
+                lds_dma16(src, to + i * NT * 16);
             }
 #pragma unroll
             for (int i = 0; i < LN; ++i) {
                 const bool up = NA && (i * NT + tid) / 8 % (BN / WN) >= BN / WN / 2;
                 const void *src = (up ? n2 : n) + no[i];
                 if (k0 + nk[i] >= k_end || (ROLE == GATED_DX && f + nk[i] >= A.F)) src = g_zeros;
-                dma16(src, to + BM * 128 + i * NT * 16);
+                lds_dma16(src, to + BM * 128 + i * NT * 16);
             }
         }
     };
@@ -476,8 +464,7 @@ tf_status gated_check(const tf_gated_config *c, int64_t n_rows) {
 }
 // A tile's rows are addressed by 32-bit offsets, its workgroups by 31-bit numbers.
 bool gated_fits(const tf_gated_config *c, int64_t n_rows, std::initializer_list<int64_t> strides) {
-    for (int64_t s : strides)
-        if (s > (1 << 22)) return false;
+    if (!strides_fit(strides, 1 << 22)) return false;
     const int64_t inner = (c->inner + 63) / 64, rows = (n_rows + 127) / 128, width = (c->width + 127) / 128;
     return inner * rows <= INT32_MAX && 2 * inner * width <= INT32_MAX && rows * width <= INT32_MAX;
 }

@@ -79,6 +79,13 @@ inline bool stride_ok(int64_t stride, int64_t width, int e) {
     return stride >= width && (stride * (int64_t)elem_bytes(e)) % 16 == 0;
 }
 
+// Whether no row stride is over what 32-bit offsets reach.
+inline bool strides_fit(std::initializer_list<int64_t> strides, int64_t most) {
+    for (int64_t s : strides)
+        if (s > most) return false;
+    return true;
+}
+
 // Whether an output is one of the inputs: workgroups would read what others have written.
 inline bool over_inputs(std::initializer_list<const void *> outputs, std::initializer_list<const void *> inputs) {
     for (const void *o : outputs)

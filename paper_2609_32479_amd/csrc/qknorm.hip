@@ -354,11 +354,7 @@ void norm_sizes(const tf_qk_norm_config *c, int64_t n_rows, NormArgs &A) {
     A.rot = c->rotary_dim, A.tile = norm_tile(c, n_rows), A.eps = c->eps, A.clear = A.offsets ? c->clear : 0;
     A.per_head[0] = per((unsigned)c->n_q_heads), A.per_head[1] = per((unsigned)c->n_k_heads), A.per_pair = per((unsigned)c->rotary_dim / 2);
 }
-bool strides_fit(std::initializer_list<int64_t> strides) {
-    for (int64_t s : strides)
-        if (s > (1 << 22)) return false;
-    return true;
-}
+constexpr int64_t kFarthest = 1 << 22;  // a tile's rows are addressed by 32-bit offsets
 
 // An output that starts at its input but whose rows lie elsewhere.
 bool in_place_elsewhere(const void *x, int64_t x_stride, const void *y, int64_t y_stride, int64_t n_rows) {
@@ -389,7 +385,7 @@ extern "C" tf_status tf_qk_norm_rotate(const tf_qk_norm_config *c, const void *q
     if (!stride_ok(q_stride, qw, c->elem) || !stride_ok(k_stride, kw, c->elem) || !stride_ok(q_out_stride, qw, c->elem) ||
         !stride_ok(k_out_stride, kw, c->elem))
         return TF_EINVAL;
-    if (!strides_fit({q_stride, k_stride, q_out_stride, k_out_stride})) return TF_EUNSUPPORTED;
+    if (!strides_fit({q_stride, k_stride, q_out_stride, k_out_stride}, kFarthest)) return TF_EUNSUPPORTED;
     if (n_rows == 0) return TF_OK;
     if (!q || !k || !q_gain || !k_gain || !q_out || !k_out) return TF_EINVAL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(q_gain) || !aligned16(k_gain) || !aligned16(q_out) || !aligned16(k_out))
@@ -421,7 +417,7 @@ extern "C" tf_status tf_qk_norm_rotate_backward(const tf_qk_norm_config *c, cons
     if (!stride_ok(q_stride, qw, c->elem) || !stride_ok(k_stride, kw, c->elem) || !stride_ok(dq_stride, qw, c->elem) ||
         !stride_ok(dk_stride, kw, c->elem) || !stride_ok(dq_out_stride, qw, c->elem) || !stride_ok(dk_out_stride, kw, c->elem))
         return TF_EINVAL;
-    if (!strides_fit({q_stride, k_stride, dq_stride, dk_stride, dq_out_stride, dk_out_stride})) return TF_EUNSUPPORTED;
+    if (!strides_fit({q_stride, k_stride, dq_stride, dk_stride, dq_out_stride, dk_out_stride}, kFarthest)) return TF_EUNSUPPORTED;
     if (!q_gain || !k_gain || !dq_gain || !dk_gain || !workspace || !aligned16(q_gain) || !aligned16(k_gain)) return TF_EINVAL;
     if (workspace_bytes < tf_qk_norm_workspace_size(c, n_rows) || ((uintptr_t)workspace & 3)) return TF_EINVAL;
     if (twice({dq, dk, dq_gain, dk_gain, workspace}) || over_inputs({workspace, dq_gain, dk_gain}, {q_gain, k_gain})) return TF_EINVAL;
