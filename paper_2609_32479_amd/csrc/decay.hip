@@ -358,6 +358,26 @@ constexpr int tile_list(int a, int b, int c, int d, int e, int f, int g, int h, 
 constexpr int kTileT = tile_list(3, 2, 1, 3, 0, 3, 2, 2, 1, 3), kTileS = tile_list(3, 2, 1, 0, 0, 2, 1, 0, 0, 1);
 __device__ __forceinline__ int tile_of(int list, int w) { return list >> (2 * w) & 3; }
 __device__ __forceinline__ int tile_at(int mt, int ms) { return mt * (mt + 1) / 2 + ms; }  // row by row
+// Values of a chunk's weights in LDS: a row tile has columns up to its diagonal, in whole fragments, padded.
+template <class M> constexpr int weights_size() { return 16 * (4 * M::PAD + (M::KM == 32 ? 192 : 160)); }
+
+// Waves a SIMD that the registers are to allow.  Not more than workgroups fit in a compute unit's LDS: asked for those, the
+// compiler gives the limit up and goes past 256 registers, which leaves one workgroup (fp32 64 x 64, 16 384 tracks of 4 heads:
+// 402 us, 272 with two; bf16 128 x 32 300 and 188).  fp32 states of d_k 128 take more registers than three or four waves leave
+// (128 x 128, one sequence of 16 384 rows: spilled 141 us, in two waves 135).  Others spill a little and are faster all the
+// same: 28 bytes or less in the 16-bit types' states of 128 x 128 (120 us, without 125), 24 in the fp32 products' outputs of 32 x 64
+// (195 us, without 208), 8 in bf16's outputs of 64 x 64.
+template <class T, int DK, int DV, int MODE> constexpr int span_waves() {
+    typedef typename MatOf<T>::M M;
+    constexpr int per = span_threads(DV) / 256, es = sizeof(typename M::E), lk = DK + M::PAD, lv = DV + M::PAD;
+    constexpr int tiles = MODE == DECAY_STATE ? lk + lv : MODE == DECAY_OUT ? 2 * lk + lv : 2 * (lk + lv);
+    constexpr int weights = MODE == DECAY_STATE ? 0 : weights_size<M>() * parts_of<M>(2);
+    constexpr int sums = MODE == DECAY_DOT ? 2 * 10 * 16 * 8 + kChunk * 4 * (DV == 32 ? 2 : DV / 16) : 0;
+    constexpr int fit = 160 * 1024 / ((kChunk * tiles + weights) * es + 2 * (int)sizeof(ChunkRows) + sums + 128) * per;
+    constexpr int want = MODE == DECAY_STATE ? (sizeof(typename T::E) == 4 && DK == 128 ? 2 : DK <= DV ? 4 : 3)
+                                             : DK * DV <= 32 * 32 || (MODE == DECAY_OUT && DK * DV <= 64 * 64) ? 3 : 2;
+    return want < fit ? want : fit;
+}
 
 // One span of one head.  A wave (four of them, eight for d_v 128) owns 16 of the state's and the output's columns (d_v 32: 16
 // of them too, and of the outputs every second row tile; its pair holds the same state); the state stays in its accumulators
@@ -372,7 +392,7 @@ __device__ __forceinline__ int tile_at(int mt, int ms) { return mt * (mt + 1) / 
 // 128 x 128, 512 workgroups: states 44 us, outputs 98 us, the matrix units a fifth and the vector units a third busy.
 // fp32: the fp32 instruction (16 times slower than bf16's) and LDS: gradients of 115 thousand rows, 4 heads of 32 x 32, 285 us.
 template <class T, int DK, int DV, int MODE>
-__global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ? 4 : 3) : DK * DV <= 32 * 32 || MODE == DECAY_OUT && DK * DV <= 64 * 64 ? 3 : 2) void tf_decay_span_kernel(DecayRuns R) {
+__global__ __launch_bounds__(span_threads(DV), (span_waves<T, DK, DV, MODE>())) void tf_decay_span_kernel(DecayRuns R) {
     typedef typename MatOf<T>::M M;
     typedef typename M::E ME;
     typedef typename M::F F;
@@ -382,7 +402,7 @@ __global__ __launch_bounds__(span_threads(DV), MODE == DECAY_STATE ? (DK <= DV ?
     // a row tile of the weights has columns up to its diagonal, in whole fragments
     auto p_ld = [](int mt) { return (16 * mt + 16 + KM - 1) / KM * KM + M::PAD; };
     auto p_at = [&](int mt) { return 16 * ((mt > 0 ? p_ld(0) : 0) + (mt > 1 ? p_ld(1) : 0) + (mt > 2 ? p_ld(2) : 0)); };
-    constexpr int PSIZE = 16 * (4 * M::PAD + (KM == 32 ? 192 : 160));
+    constexpr int PSIZE = weights_size<M>();
     constexpr int RG = DV == 32 ? 2 : 1, TM = 4 / RG;  // waves that share a column tile, and their row tiles
     constexpr int ST = DK / 16;                    // state tiles of a wave's column tile
     constexpr int NB = kChunk / KM;                // fragments along a chunk's rows
