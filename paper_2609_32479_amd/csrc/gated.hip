@@ -471,9 +471,13 @@ bool gated_fits(const tf_gated_config *c, int64_t n_rows, std::initializer_list<
 int64_t gated_pad(const tf_gated_config *c) { return ((int64_t)c->inner + 63) / 64 * 64; }
 
 // The tiles of a product of m x n: 256 x 256, one workgroup of eight waves a compute unit, or 128 x 128, two of four waves,
-// each with a ring of two stages (and 64 x 64 for few tiles, below).  Whole rounds of the compute units' tiles are paid for; a round of pairs of small tiles
-// takes 0.62 of one of large ones, for half its products.  5003 x 1032 with sums of 5504: 77 us in small tiles, 126 in
-// large ones; 256 x 128 with three stages and 128 x 128 with four, one workgroup a compute unit: 88 and 124.
+// each with a ring of two stages (and 64 x 64 for few tiles, below).  16-bit types: whole rounds of the compute units' tiles are
+// paid for; a round of pairs of small tiles takes 0.62 of one of large ones, for half its products.  5003 x 1032 with sums of 5504:
+// 77 us in small tiles, 126 in large ones; 256 x 128 with three stages and 128 x 128 with four, one workgroup a compute unit: 88
+// and 124.  Forward and backward at 43 shapes of 1500 to 14 000 rows, 512 to 2048 -> 1024 to 5600, the rule is level with the
+// better of the two on average and 10 % over it at worst, where small tiles alone lose up to 16 and large ones alone up to 57 %.
+// fp32, whose products take sixteen times as long: small tiles, as fast or faster at all of 28 shapes (700 x 1024 -> 2 x 5600
+// forward: 193 us for 242).
 constexpr int kShapes[3] = {256, 128, 64};
 constexpr double kRound[2] = {1.0, 0.62};
 // Tiles of 128 x 128 up to which the projections, whose sums are not split, take 64 x 64 (up to five workgroups a compute unit):
@@ -541,8 +545,13 @@ template <class T, int ROLE, bool GELU> void gated_product(const GatedArgs &A, i
             return;
         }
     }
-    if (gated_shape(A.M, n) == 0) gated_tile<T, ROLE, 0, GELU, false>(A, 1, s);
-    else gated_tile<T, ROLE, 1, GELU, false>(A, 1, s);
+    if constexpr (sizeof(typename T::E) == 2) {
+        if (gated_shape(A.M, n) == 0) {
+            gated_tile<T, ROLE, 0, GELU, false>(A, 1, s);
+            return;
+        }
+    }
+    gated_tile<T, ROLE, 1, GELU, false>(A, 1, s);
 }
 template <class T, bool BACK, bool GELU> void gated_project(const GatedArgs &A, hipStream_t s) {
     if (A.M <= kFewRows) {
