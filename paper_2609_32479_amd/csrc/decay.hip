@@ -387,10 +387,11 @@ template <class T, int DK, int DV, int MODE> constexpr int span_waves() {
 //
 // Chunks of 64 rows: a chunk's weights cost 64 (d_k + d_v) products a row and its state 2 d_k d_v, equal at 64 columns, and
 // tracks of up to 20 hits are whole within one or two.  What bounds it: with many spans, memory.  918 161 rows of 65 536 tracks,
-// 3 heads of 64 x 64, bf16: 1.42 GB in 342 us, 4.2 TB/s of the 5.1 that a copy reaches, the vector units 42 % busy.  With few,
-// the latency of a chunk's phases, each behind a barrier (about 7 us a chunk at 2 GHz): one sequence of 32 768 rows, 8 heads of
-// 128 x 128, 512 workgroups: states 44 us, outputs 98 us, the matrix units a fifth and the vector units a third busy.
-// fp32: the fp32 instruction (16 times slower than bf16's) and LDS: gradients of 115 thousand rows, 4 heads of 32 x 32, 285 us.
+// 3 heads of 64 x 64, bf16: 1.42 GB in 357 us, 4.0 TB/s of the 5.1 that a copy reaches, the vector units half busy.  With few,
+// the latency of a chunk's phases, each behind a barrier: one sequence of 32 768 rows, 8 heads of 128 x 128, 512 workgroups of
+// eight chunks, 161 us.  The states, two workgroups a compute unit, take 47 us, 6 a chunk; the outputs, whose registers leave one
+// workgroup a compute unit and so two rounds, 109 us, 7 a chunk; the matrix units a fifth and the vector units two fifths busy.
+// fp32: the fp32 instruction (16 times slower than bf16's) and LDS: gradients of 115 thousand rows, 4 heads of 32 x 32, 280 us.
 template <class T, int DK, int DV, int MODE>
 __global__ __launch_bounds__(span_threads(DV), (span_waves<T, DK, DV, MODE>())) void tf_decay_span_kernel(DecayRuns R) {
     typedef typename MatOf<T>::M M;
@@ -1187,10 +1188,10 @@ tf_status decay_check(const tf_decay_config *c) {
     return TF_OK;
 }
 
-// Rows of a span.  Enough spans that the compute units have four workgroups each (two of the wide heads', which hold
-// fewer), and no more than that: every border that cuts a sequence costs a state written and read.  One sequence of 32 768 rows,
-// 8 heads of 128 x 128: spans of 128 rows 239 us, 256 194, 512 157, 1024 154.  Not beyond 512 rows: the last workgroups' share of
-// 918 161 rows of tracks grows (spans of 512 362 us, 1024 367, 2048 373).
+// Rows of a span.  Four workgroups for each compute unit (two of the wide heads'), of which an instance's registers and LDS let
+// three, two or one run at a time, and no more than that: every border that cuts a sequence costs a state written and read.  One
+// sequence of 32 768 rows, 8 heads of 128 x 128: spans of 128 rows 239 us, 256 194, 512 157, 1024 154.  Not beyond 512 rows: the
+// last workgroups' share of 918 161 rows of tracks grows (spans of 512 362 us, 1024 367, 2048 373).
 int decay_span(const tf_decay_config *c, int64_t n_rows) {
     int64_t s = n_rows * c->n_heads / (c->d_k * c->d_v > 64 * 64 ? 512 : 1024) / kChunk * kChunk;
     if (s < kMinSpan) s = kMinSpan;
@@ -1441,7 +1442,7 @@ extern "C" tf_status tf_decay_attention_backward(const tf_decay_config *c, const
         V.q = k, V.qs = k_stride, V.qg = 1;
         V.out = dv, V.os = dv_stride;
         V.sf = d_initial, V.sf_decay = 1;
-        if (c->d_k == c->d_v) {  // (9.6 thousand rows, which leave compute units idle: together 73 us, apart 59 and 27)
+        if (c->d_k == c->d_v) {  // (9.6 thousand rows, which leave compute units idle: together 75 us, apart 59 and 27)
             V.x = nullptr;
             span_run(c->elem, {{Q, K, V}}, 3, c->d_k, c->d_v, DECAY_DOT, stream);
         } else {

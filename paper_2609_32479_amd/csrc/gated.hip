@@ -22,9 +22,11 @@
 // consecutive values of a token.
 //
 // What bounds it: the matrix units and the LDS reads that feed them.  16 384 x 2048 -> 2 x 5632, bf16: 608 to 617 us, 1225 to 1243 TFLOP/s
-// (a library product of 8192 cubed reaches 1363), no LDS bank conflicts, 59 % of the cycles with a matrix instruction under way.
-// Backward at 5003 x 1032 -> 2731, GELU: 93 us for the projections and their gradients, 78 and 76 for the two products, which
-// fill 360 and 387 of the 512 places for small tiles.
+// (a library product of 8192 cubed reaches 1363), no LDS bank conflicts, 58 % of the cycles with a matrix instruction under way.
+// Backward at 5003 x 1032 -> 2731, GELU: 92 us for the projections and their gradients, 77 and 75 for the two products, which
+// fill 360 and 387 of the 512 places for small tiles.  da and db are rounded to the tensors' type, as their products' operands are:
+// in 16-bit types dx and the weights' gradients are off by 1.4 times the rounding at the store (bf16, two-norms: 2.3e-3 for
+// 1.7e-3).  In two parts each they would not be, and the two products would take twice as long, the call about 380 us for 226.
 //
 // Few tokens (up to 64): reading the weights bounds it.  tf_gated_rows_kernel
 // streams them once, straight to registers, the sum dealt out to a workgroup's

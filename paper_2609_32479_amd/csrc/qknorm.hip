@@ -18,10 +18,10 @@
 // good to 2^-23 turns, where an fp32 angle has lost whole turns.
 // Everything between the loads and the one rounding at the store is fp32.
 //
-// Memory bounds it: 918 thousand rows of 3 + 3 heads of 64, bf16, 1.41 GB in 310 us (4.5 TB/s; a copy reaches 5.1), and
-// backward 22 thousand rows of 16 + 4 heads of 128, 342 MB in 90 us (3.8 TB/s), 7 of them the gains' sums, whose launch is
+// Memory bounds it: 918 thousand rows of 3 + 3 heads of 64, bf16, 1.41 GB in 315 us (4.5 TB/s; a copy reaches 5.1), and
+// backward 22 thousand rows of 16 + 4 heads of 128, 342 MB in 89 us (3.8 TB/s), 8 of them the gains' sums, whose launch is
 // latency.  16 values a lane: a lane then has both halves of its pairs in two or four 16-byte loads, and a head's sums are two
-// to four exchanges; 32 registers of gains' sums still leave the backward pass its four workgroups a compute unit.
+// to four exchanges; with 32 registers of gains' sums the backward pass has three workgroups a compute unit.
 #include "ops.h"
 
 #include <cmath>
@@ -291,7 +291,8 @@ __global__ __launch_bounds__(1024) void tf_qk_norm_gain_kernel(const float *__re
 }
 
 // Rows of a tile: as many angles as the LDS array holds, fewer where that leaves compute units without a tile; and so
-// that the tiles come out even for 1024 workgroups (the backward pass has no more; 1059 tiles took it twice 1024's time).
+// that the tiles come out even for 1024 workgroups (the backward pass has no more; 1059 tiles took it twice 1024's time; 768 of
+// them run at a time).
 int norm_tile(const tf_qk_norm_config *c, int64_t n_rows) {
     const int64_t most = kNormAngles / (c->rotary_dim / 2);
     const int64_t rounds = (n_rows + 1024 * most - 1) / (1024 * most);
