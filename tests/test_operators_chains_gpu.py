@@ -183,3 +183,22 @@ def test_decays_gradient_of_heads_that_forget_at_once_with_states(tf, dtype, fir
     err = (got - want).abs().max().item()
     print(f"[fast] {dtype} {first} {reverse}: {err:.2e} of {bound:.2e}, largest gradient {want.abs().max().item():.2e}", flush=True)
     assert err <= bound < want.abs().max().item() / 4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, FP32, FP16])
+@pytest.mark.parametrize("reverse,states", [(False, False), (True, True)])
+def test_gradient_of_one_decay_a_head(tf, dtype, reverse, states):
+    """log_decay of one value a head: the sum of the rows' gradients over all sequences, cut ones among them."""
+    t, off = _inputs(59, dtype, [900, 1, 0, 20, 65], 4, 2, 64, 32, "mixed", 5, 3)
+    one = -0.6 * 4.0 ** -torch.arange(4).float()
+    t["g"] = one.expand(t["g"].shape).contiguous()
+    rows = _ref(t, off, 0.125, reverse, states)["dg"][off[0]:off[-1]]
+    c, o = {k: x.cuda() for k, x in t.items()}, torch.from_numpy(off).cuda()
+    got = tf.decay_attention_backward(c["d_out"], c["q"], c["k"], c["v"], one.cuda(), o, scale=0.125, reverse=reverse,
+                                      initial_state=c["s0"] if states else None, d_state=c["d_state"] if states else None)[3].double().cpu()
+    want = rows.sum(0)
+    # the rows' gradients are off by NORM_FP32 in the two-norm: their sum by at most that times the root of their number
+    bound = forms.NORM_FP32 * rows.norm(dim=0) * len(rows) ** 0.5
+    print(f"[one decay] {dtype} {(got - want).abs().tolist()} of {bound.tolist()}, {want.tolist()}", flush=True)
+    assert bool(((got - want).abs() <= bound).all()) and bool((bound < want.abs() / 4).all())
